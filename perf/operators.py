@@ -201,12 +201,12 @@ def _prepare_router(c, seed):
         s["dlogits"] = torch.empty_like(s["logits"])
         s["loss"] = torch.empty(c["layers"], 2, device="cuda")
         s["counts"] = _counts(s)
-    if own:      # what a program makes once: the set of its routers' tensors, a workspace
+    if own:      # what a program makes once: the set of its routers' tensors and a workspace
         from paper_2004_13336_b200 import binding as ws
         valid = None if s["valid"] is None else [s["valid"][a:b] for a, b in zip(bounds, bounds[1:])]
         more = {} if c["op"] == "counts" else {"logits": cut(s["logits"]), "dlogits": cut(s["dlogits"]), "score": c["score"]}
         s["routers"] = ws.RouterSet(experts, cut(s["picks"]), valid=valid, **more)
-        s["workspace"] = torch.zeros(s["routers"].workspace_bytes(), dtype=torch.uint8, device="cuda")
+        s["workspace"] = torch.empty(s["routers"].workspace_bytes(), dtype=torch.uint8, device="cuda")
     return s
 
 
@@ -331,7 +331,7 @@ def run(s):
         ws.ws_reduce_dropout(s["plan"], -1, s["table"], ws.make_dropout(c["p"], s["seed"], c["step"], c["replica"]), s["flat"])
         return s["flat"]
     if c["op"] == "counts":
-        ws.ws_router_counts(s["routers"], s["counts"], workspace=s["workspace"])
+        ws.ws_router_counts(s["routers"], s["counts"])
         return s["counts"]
     ws.ws_balance_loss(s["routers"], s["counts"], s["loss"], 1e-2, z_coef=c["z"], workspace=s["workspace"])
     return {"loss": s["loss"], "dlogits": s["dlogits"]}
