@@ -578,6 +578,116 @@ ws_status ws_lamb_update_static_scratch(const ws_plan* plan, const ws_grads* gra
                                         const ws_state* state, const ws_hyper* hyper,
                                         const ws_out* out, void* stream);
 
+/* ------------------------------------ dropout of the replicas' weights ---
+ * Every replica trains on its own random part of the weights: replica k's copy of tensor t is
+ *   W_k[t][i] = keep(k, t, i) w[t][i] / (1 - p),
+ * and the gradient of the shared weights is the same masks' sum over the replicas' gradients,
+ *   g[t][i] = sum_k keep(k, t, i) g_k[t][i] / (1 - p).
+ * (No counterpart in the paper; the hand-out stands where ws_unpack stands after the all-gather of
+ * Section 4.2, the sum where ws_pack and the reduce-scatter's sum stand, Sections 2.2 and 5.1.)
+ * No mask is ever stored: both calls draw it from a counter-based generator, Philox4x32 with 7 rounds
+ * (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011: the smallest number of
+ * rounds that passes every test of its battery).  Elements 8 j ... 8 j + 7 of tensor t take the 8 16-bit halves (low half
+ * first) of the four words that
+ *   key     = (low, high 32 bits of seed)
+ *   counter = (low 32 bits of j, step, t, replica + 2^16 (j / 2^32))
+ * give, and an element is kept where its half is >= T = min(floor(65536 p + 1/2), 65535).  The scale is
+ * 65536 / (65536 - T), so the expectation of a copy is the weight exactly.  The masks depend on none of the
+ * plan's choices: the same for every shard count, layout, alignment, tile length and data type.
+ *   p         0 <= p < 1
+ *   seed      of the run; step of the training step (any values)
+ *   replica   number of the table's first set: set k belongs to replica + k.  0 <= replica, and
+ *             replica + nsets <= 65536
+ *   step_dev  device word (4-byte aligned) that is added to step when the kernels run, modulo 2^32, or
+ *             NULL: a captured step draws new masks at each replay if the word is counted up in between
+ * A dropped element reads nothing into its result: infinities and NaN there leave no trace.
+ * ws_unpack_dropout hands out `flat` ([R][S], the fp32 state or a gathered copy of either type) to every
+ * set of `lists`, rounded once to the tables' type (nearest-even); pads are not read.
+ * ws_reduce_dropout writes the masked and scaled sum of all sets of `grads` to `flat` ([R][S], of either
+ * type), pads as +0: one gradient copy for ws_shard_update, or with one set what a replica gives to its
+ * reduce-scatter.  The sum is formed in fp32, up to 8 sets in any order, more with compensation, scaled and
+ * rounded once; a sum that an infinity enters is infinite.
+ *   r         -1: all shards.  r >= 0: shard r alone, `flat` is its S elements (the tensors' other elements
+ *             are neither read nor written)
+ * Tables as for ws_fused_update, 1 to 1024 sets.  The sets' tensors are distinct memory. */
+typedef struct {
+    double p;
+    uint64_t seed;
+    uint32_t step;
+    int32_t replica;
+    const uint32_t* step_dev;
+} ws_dropout;
+
+ws_status ws_unpack_dropout(const ws_plan* plan, int32_t r, const void* flat, ws_dtype flat_dtype,
+                            const ws_tensor_table* lists, const ws_dropout* drop, void* stream);
+ws_status ws_reduce_dropout(const ws_plan* plan, int32_t r, const ws_tensor_table* grads,
+                            const ws_dropout* drop, void* flat, ws_dtype flat_dtype, void* stream);
+
+/* ------------------------------------------- balance of a model's experts ---
+ * A mixture-of-experts layer's router gives every token a row of logits, one per expert, and the token goes
+ * to the experts of its topk picks.  The balance of the load is a property of the whole batch, so its
+ * statistics are sums over the replicas, like the norms of Section 4.1 ("Non-elementwise operators"):
+ *   c[l][e]  number of picks of expert e in layer l over all valid tokens of all replicas,
+ *   N[l]     number of those tokens,             f_e = c_e / (topk N)
+ *   p_n      scores of token n: WS_SOFTMAX of its logits, or WS_SIGMOID, p_ne = s_ne / sum_j s_nj with
+ *            s = 1 / (1 + exp(-x))
+ *   loss[l][0] = coef experts / N  sum_n sum_e f_e p_ne
+ *   loss[l][1] = z_coef / N  sum_n lse_n^2,       lse_n = log sum_e exp x_ne  (WS_SOFTMAX only)
+ * and, the counts being constants, the gradient of u (loss[l][0] + loss[l][1]) by the logits is
+ *   p_e (u coef experts / N (f_e - sum_j f_j p_j) + 2 u z_coef / N lse)           (WS_SOFTMAX)
+ *   p_e  u coef experts / N (f_e - sum_j f_j p_j) (1 - s_e)                       (WS_SIGMOID).
+ * It needs the counts and the token's own row only, so loss and gradient are one pass over the logits.
+ * On real replicas each counts its own tokens, an all-reduce sums the counts, each runs ws_balance_loss on
+ * its own logits, and the losses' sum over the replicas is the loss of the batch.
+ *
+ * ws_router_set names the routers' tensors of a step; its arrays are host arrays, read before a call returns.
+ *   layers    1 ... 65535;  replicas 1 ... 512;  experts 1 ... 1024;  topk 1 ... experts
+ *   tokens    [replicas] tokens of every replica, 0 ... 2^31 - 1, the same in all layers
+ *   picks     [layers][replicas] device pointers to [tokens][topk] integers of index_bytes (4 or 8) bytes,
+ *             contiguous.  A number outside 0 ... experts - 1 is no pick (a token that a full expert
+ *             refused); one that stands in a row twice counts twice
+ *   valid     NULL, or [replicas] device pointers (or NULL) to [tokens] bytes: a token with byte 0 does not
+ *             exist (the end of a padded sequence): its picks do not count, its logits are not read (they may hold
+ *             NaN) and their gradient is 0
+ *   logits    [layers][replicas] device pointers to [tokens] rows of `experts` elements of `dtype`, row n at
+ *             n * logits_ld (>= experts) elements
+ *   dlogits   the gradients' rows, likewise with dlogits_ld; NULL for the loss alone.  May be the logits.
+ * Pointers are aligned to their elements; rows on 16-byte boundaries take the vectors' path.  A pointer of a
+ * replica without tokens is not read and may be NULL; so may picks in ws_balance_loss and logits and dlogits in
+ * ws_router_counts.
+ *
+ * ws_router_counts writes counts[l][0 ... experts - 1] = c and counts[l][experts] = N (device, int64,
+ * [layers][experts + 1]); with `accumulate` it adds to them (several microbatches of one step).
+ * ws_balance_loss reads them and writes loss ([layers][2] floats, device, or NULL) and dlogits; with
+ * `accumulate` it adds the gradient to what dlogits holds (in fp32, rounded once).  A logit of -infinity is
+ * an expert that the token cannot pick, with score and gradient 0; a row of nothing else has no scores, adds
+ * nothing to either loss and has gradient 0.  NaN or (WS_SOFTMAX) +infinity in a valid row gives NaN.  A layer
+ * without tokens has loss and gradient 0.
+ *   coef, z_coef  finite; z_coef must be 0 with WS_SIGMOID
+ *   upstream      device float u, or NULL for 1
+ *   workspace     device scratch of ws_balance_workspace_bytes(set) bytes, 16-byte aligned; nothing in it
+ *                 has to be cleared.  Calls that can run at the same time need one each.
+ * Sums over tokens are formed in 64 bits in a fixed order: the same call gives the same bits. */
+typedef enum { WS_SOFTMAX = 0, WS_SIGMOID = 1 } ws_score;
+typedef struct {
+    int32_t layers, replicas, experts, topk;
+    const int64_t* tokens;
+    const void* const* picks;
+    const uint8_t* const* valid;
+    const void* const* logits;
+    void* const* dlogits;
+    int64_t logits_ld, dlogits_ld;
+    int32_t index_bytes;
+    ws_dtype dtype;
+    ws_score score;
+} ws_router_set;
+
+ws_status ws_router_counts(const ws_router_set* set, int64_t* counts, int32_t accumulate, void* stream);
+size_t ws_balance_workspace_bytes(const ws_router_set* set); /* 0 for a set that ws_balance_loss refuses */
+ws_status ws_balance_loss(const ws_router_set* set, const int64_t* counts, float* loss, double coef,
+                          double z_coef, const float* upstream, int32_t accumulate, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
 /* ---------------------------------------------- bounds-checking debug build ---
  * (Test infrastructure of the library, no counterpart in the paper.)  A copy of the library
  * compiled with -DWS_DEBUG_BOUNDS (`python -m paper_2004_13336_b200.build --debug` builds it as

@@ -28,6 +28,8 @@ OPT_CODE = {"sgdm": WS_SGDM, "adam": WS_ADAM, "lamb": WS_LAMB, "lars": WS_LARS, 
 WS_LAYOUT_PER_TENSOR, WS_LAYOUT_CONCAT = 0, 1
 LAYOUT_CODE = {"per_tensor": WS_LAYOUT_PER_TENSOR, "concat": WS_LAYOUT_CONCAT}
 WS_MAX_DIMS = 8
+WS_SOFTMAX, WS_SIGMOID = 0, 1
+SCORE_CODE = {"softmax": WS_SOFTMAX, "sigmoid": WS_SIGMOID}
 
 
 class WsError(RuntimeError):
@@ -71,6 +73,18 @@ class ws_tensor_table(C.Structure):
                 ("min_align", C.c_int32)]
 
 
+class ws_dropout(C.Structure):
+    _fields_ = [("p", C.c_double), ("seed", C.c_uint64), ("step", C.c_uint32), ("replica", C.c_int32),
+                ("step_dev", C.c_void_p)]
+
+
+class ws_router_set(C.Structure):
+    _fields_ = [("layers", C.c_int32), ("replicas", C.c_int32), ("experts", C.c_int32), ("topk", C.c_int32),
+                ("tokens", C.POINTER(C.c_int64)), ("picks", C.POINTER(C.c_void_p)), ("valid", C.POINTER(C.c_void_p)),
+                ("logits", C.POINTER(C.c_void_p)), ("dlogits", C.POINTER(C.c_void_p)), ("logits_ld", C.c_int64),
+                ("dlogits_ld", C.c_int64), ("index_bytes", C.c_int32), ("dtype", C.c_int32), ("score", C.c_int32)]
+
+
 class ws_sched_item(C.Structure):
     _fields_ = [("tensor", C.c_int32), ("shard", C.c_int32), ("pos", C.c_int64), ("tensor_off", C.c_int64),
                 ("len", C.c_int32), ("nvalid", C.c_int32)]
@@ -96,6 +110,8 @@ EXPORTS = [
     "ws_adafactor_stage", "ws_workspace_adafactor_sums",
     "ws_plan_schedule_bytes", "ws_plan_upload_schedule", "ws_plan_schedule_view", "ws_plan_schedule_item",
     "ws_workspace_sync_status", "ws_plan_one_kernel",
+    "ws_unpack_dropout", "ws_reduce_dropout",
+    "ws_router_counts", "ws_balance_workspace_bytes", "ws_balance_loss",
     "ws_debug_bounds_enabled", "ws_debug_bounds_read", "ws_debug_bounds_selftest",
 ]
 
@@ -191,6 +207,16 @@ def lib() -> C.CDLL:
     L.ws_fused_update.restype = C.c_int
     L.ws_fused_update.argtypes = [vp, C.c_int32, C.POINTER(ws_tensor_table), C.POINTER(ws_state),
                                   C.POINTER(ws_hyper), C.POINTER(ws_tensor_table), vp, C.c_size_t, vp]
+    L.ws_unpack_dropout.restype = C.c_int
+    L.ws_unpack_dropout.argtypes = [vp, C.c_int32, vp, C.c_int, C.POINTER(ws_tensor_table), C.POINTER(ws_dropout), vp]
+    L.ws_reduce_dropout.restype = C.c_int
+    L.ws_reduce_dropout.argtypes = [vp, C.c_int32, C.POINTER(ws_tensor_table), C.POINTER(ws_dropout), vp, C.c_int, vp]
+    L.ws_router_counts.restype = C.c_int
+    L.ws_router_counts.argtypes = [C.POINTER(ws_router_set), vp, C.c_int32, vp]
+    L.ws_balance_workspace_bytes.restype = C.c_size_t
+    L.ws_balance_workspace_bytes.argtypes = [C.POINTER(ws_router_set)]
+    L.ws_balance_loss.restype = C.c_int
+    L.ws_balance_loss.argtypes = [C.POINTER(ws_router_set), vp, vp, C.c_double, C.c_double, vp, C.c_int32, vp, C.c_size_t, vp]
     L.ws_plan_schedule_bytes.restype = C.c_size_t
     L.ws_plan_schedule_bytes.argtypes = [vp]
     L.ws_plan_upload_schedule.restype = C.c_int
@@ -231,7 +257,11 @@ def _step():
         for name, args in (("ws_pack", [vp, vp, C.c_int, vp, vp]), ("ws_unpack", [vp, vp, C.c_int, vp, vp]),
                            ("ws_pack_sets", [vp, vp, vp, vp]),
                            ("ws_shard_update", [vp, i32, vp, vp, vp, vp, vp, size, vp]),
-                           ("ws_fused_update", [vp, i32, vp, vp, vp, vp, vp, size, vp])):
+                           ("ws_fused_update", [vp, i32, vp, vp, vp, vp, vp, size, vp]),
+                           ("ws_unpack_dropout", [vp, i32, vp, C.c_int, vp, vp, vp]),
+                           ("ws_reduce_dropout", [vp, i32, vp, vp, vp, C.c_int, vp]),
+                           ("ws_router_counts", [vp, vp, i32, vp]),
+                           ("ws_balance_loss", [vp, vp, vp, C.c_double, C.c_double, vp, i32, vp, size, vp])):
             f = getattr(S, name)
             f.restype = C.c_int
             f.argtypes = args
@@ -679,3 +709,166 @@ def ws_pack_sets(plan: Plan, table: TensorTable, flats):
     st = _step().ws_pack_sets(plan.handle, C.addressof(table.c), addr, _stream())
     if st:
         raise WsError(st, "ws_pack_sets")
+
+
+def make_dropout(p: float, seed: int, step: int = 0, replica: int = 0,
+                 step_dev: Optional[torch.Tensor] = None) -> ws_dropout:
+    """Dropout of probability ``p`` for ws_unpack_dropout and ws_reduce_dropout: masks of the run ``seed`` and the
+    training step ``step``; a table's first set belongs to ``replica``.  ``step_dev``: a device tensor of one 32-bit
+    integer that the kernels add to ``step``, for captured steps; the caller keeps it alive."""
+    if step_dev is not None:
+        if step_dev.dtype not in (torch.int32, torch.uint32) or step_dev.numel() != 1 or not step_dev.is_cuda:
+            raise TypeError("step_dev is a device tensor of one 32-bit integer")
+    d = ws_dropout(float(p), int(seed) & 0xFFFFFFFFFFFFFFFF, int(step) & 0xFFFFFFFF, int(replica),
+                   step_dev.data_ptr() if step_dev is not None else None)
+    d._keep = step_dev
+    return d
+
+
+def _on_current_device(t):
+    """The calls launch on the current device's current stream: a tensor of another device has no place there."""
+    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"a tensor on the current device expected, not on {t.device}")
+
+
+def _check_flat(plan, r, flat):
+    """ws_unpack_dropout and ws_reduce_dropout take a whole layout or one shard by ``r``: its size is all that tells a
+    buffer of the other kind from the right one."""
+    _on_current_device(flat)
+    want = plan.G if r < 0 else plan.S
+    if flat.numel() != want or not flat.is_contiguous():
+        raise ValueError(f"flat is a contiguous buffer of {want} elements for r = {r}, not {tuple(flat.shape)}")
+
+
+def ws_unpack_dropout(plan: Plan, r: int, flat: torch.Tensor, lists: TensorTable, drop: ws_dropout):
+    """Hands ``flat`` ([R][S], or shard ``r`` of it) out to every set of ``lists``, each under its own dropout mask."""
+    if type(lists.c) is not ws_tensor_table or type(drop) is not ws_dropout:
+        for x, cls in ((lists.c, ws_tensor_table), (drop, ws_dropout)):
+            _refuse(x, cls)
+    _check_flat(plan, r, flat)
+    st = _step().ws_unpack_dropout(plan.handle, r, flat.data_ptr(), _dtype_code(flat.dtype), C.addressof(lists.c),
+                                   C.addressof(drop), _stream())
+    if st:
+        raise WsError(st, "ws_unpack_dropout")
+
+
+def ws_reduce_dropout(plan: Plan, r: int, grads: TensorTable, drop: ws_dropout, flat: torch.Tensor):
+    """Sum of every set of ``grads`` under the masks of ws_unpack_dropout, into ``flat`` ([R][S], or shard ``r`` of it)."""
+    if type(grads.c) is not ws_tensor_table or type(drop) is not ws_dropout:
+        for x, cls in ((grads.c, ws_tensor_table), (drop, ws_dropout)):
+            _refuse(x, cls)
+    _check_flat(plan, r, flat)
+    st = _step().ws_reduce_dropout(plan.handle, r, C.addressof(grads.c), C.addressof(drop), flat.data_ptr(),
+                                   _dtype_code(flat.dtype), _stream())
+    if st:
+        raise WsError(st, "ws_reduce_dropout")
+
+
+class RouterSet:
+    """The routers' tensors of a training step for ws_router_counts and ws_balance_loss: nested lists, one inner list per
+    layer with one tensor per replica.  ``picks``: integers [tokens, topk]; ``logits`` and ``dlogits``: [tokens, experts]
+    with contiguous rows (a common row stride); ``valid``: None, or one bool or byte tensor [tokens] (or None) per
+    replica.  Keeps the tensors and the C arrays, so that a call of every step costs one ctypes call."""
+
+    def __init__(self, experts: int, picks=None, valid=None, logits=None, dlogits=None, score: str = "softmax"):
+        like = picks if picks is not None else logits
+        if not like or not like[0]:
+            raise ValueError("a router set has picks or logits of one layer and one replica at least")
+        layers, replicas = len(like), len(like[0])
+        tokens = [t.shape[0] for t in like[0]]
+        self.experts, self.layers, self.replicas = int(experts), layers, replicas
+        self.device = like[0][0].device
+        c = self.c = ws_router_set(layers=layers, replicas=replicas, experts=experts, topk=1)
+        self._keep = keep = []
+
+        def table(name, lists, width):
+            if len(lists) != layers or any(len(x) != replicas for x in lists):
+                raise ValueError(f"{name}: one list per layer with one tensor per replica")
+            flat = [t for x in lists for t in x]
+            for i, t in enumerate(flat):
+                if t.dim() != 2 or t.shape[0] != tokens[i % replicas] or t.shape[1] != width:
+                    raise ValueError(f"{name}: [{tokens[i % replicas]}, {width}] expected, not {tuple(t.shape)}")
+                if t.dtype != flat[0].dtype or t.device != self.device:
+                    raise ValueError(f"{name}: tensors of one type on one device")
+            arr = _ptr_array(flat)
+            keep.extend((flat, arr))
+            return flat, C.cast(arr, C.POINTER(C.c_void_p))
+
+        def stride(name, flat):
+            """Elements from row to row, the same for all tensors of more than one row."""
+            lds = {t.stride(0) for t in flat if t.shape[0] > 1} or {max(1, experts)}
+            if len(lds) > 1 or any(experts > 1 and t.numel() and t.stride(1) != 1 for t in flat):
+                raise ValueError(f"{name}: contiguous rows at one stride expected")
+            return lds.pop()
+
+        if picks is not None:
+            c.topk = picks[0][0].shape[1]
+            flat, c.picks = table("picks", picks, c.topk)
+            if flat[0].dtype not in (torch.int32, torch.int64) or not all(t.is_contiguous() for t in flat):
+                raise TypeError("picks: contiguous int32 or int64 tensors")
+            c.index_bytes = flat[0].element_size()
+        if logits is not None:
+            flat, c.logits = table("logits", logits, experts)
+            c.dtype, c.logits_ld, c.score = _dtype_code(flat[0].dtype), stride("logits", flat), SCORE_CODE[score]
+            if dlogits is not None:
+                grads, c.dlogits = table("dlogits", dlogits, experts)
+                if grads[0].dtype != flat[0].dtype:
+                    raise TypeError("dlogits: the type of the logits")
+                c.dlogits_ld = stride("dlogits", grads)
+        elif dlogits is not None:
+            raise ValueError("dlogits without logits")
+        if valid is not None:
+            if len(valid) != replicas:
+                raise ValueError("valid: one tensor (or None) per replica")
+            arr = (C.c_void_p * replicas)()
+            for k, t in enumerate(valid):
+                if t is None:
+                    continue
+                if t.dtype not in (torch.bool, torch.uint8) or tuple(t.shape) != (tokens[k],) or not t.is_contiguous() or t.device != self.device:
+                    raise ValueError("valid: contiguous bool or byte tensors, one element per token")
+                arr[k] = t.data_ptr()
+            keep.extend((list(valid), arr))
+            c.valid = C.cast(arr, C.POINTER(C.c_void_p))
+        self._tokens = (C.c_int64 * replicas)(*tokens)
+        c.tokens = C.cast(self._tokens, C.POINTER(C.c_int64))
+        self.addr = C.addressof(c)
+
+    def workspace_bytes(self) -> int:
+        """Bytes of scratch that ws_balance_loss needs (0 for a set without logits)."""
+        return lib().ws_balance_workspace_bytes(C.byref(self.c))
+
+
+def _router_addr(routers, counts):
+    if not isinstance(routers, RouterSet):
+        raise TypeError(f"expected RouterSet instead of {type(routers).__name__}")
+    if (counts.dtype != torch.int64 or tuple(counts.shape) != (routers.layers, routers.experts + 1) or not counts.is_contiguous()
+            or counts.device != routers.device):
+        raise ValueError(f"counts: a contiguous int64 tensor [{routers.layers}, {routers.experts + 1}] beside the routers' tensors")
+    _on_current_device(counts)
+    return routers.addr
+
+
+def ws_router_counts(routers: RouterSet, counts: torch.Tensor, accumulate: bool = False):
+    """counts[l] = picks of every expert of layer l over all replicas' valid tokens, and as its last entry their number
+    (``accumulate``: added to what counts holds)."""
+    st = _step().ws_router_counts(_router_addr(routers, counts), counts.data_ptr(), 1 if accumulate else 0, _stream())
+    if st:
+        raise WsError(st, "ws_router_counts")
+
+
+def ws_balance_loss(routers: RouterSet, counts: torch.Tensor, loss: Optional[torch.Tensor], coef: float, z_coef: float = 0.0,
+                    upstream: Optional[torch.Tensor] = None, accumulate: bool = False,
+                    workspace: Optional[torch.Tensor] = None):
+    """The load-balancing loss and the z loss of every layer (loss[l][0], loss[l][1]) and, into the set's dlogits, the
+    gradient of ``upstream`` (a device float, else 1) times their sum by the logits."""
+    addr = _router_addr(routers, counts)
+    if loss is not None and (loss.dtype != torch.float32 or tuple(loss.shape) != (routers.layers, 2) or not loss.is_contiguous()):
+        raise ValueError(f"loss: a contiguous float32 tensor [{routers.layers}, 2]")
+    if upstream is not None and (upstream.dtype != torch.float32 or upstream.numel() != 1 or not upstream.is_cuda):
+        raise TypeError("upstream: a device tensor of one float32")
+    st = _step().ws_balance_loss(addr, counts.data_ptr(), loss.data_ptr() if loss is not None else None, coef, z_coef,
+                                 upstream.data_ptr() if upstream is not None else None, 1 if accumulate else 0,
+                                 workspace.data_ptr() if workspace is not None else None,
+                                 workspace.nbytes if workspace is not None else 0, _stream())
+    if st:
+        raise WsError(st, "ws_balance_loss")
