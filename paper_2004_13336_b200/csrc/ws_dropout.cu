@@ -53,6 +53,13 @@ __device__ __forceinline__ bool kept(const uint4& w, int i, unsigned thr) {
     return (i & 1 ? x : x << 16) >= thr;
 }
 
+// sum += x where element i of the block is kept: an addition under a predicate, without a choice in front of it (the
+// integer and choice instructions are what these kernels have most of).
+__device__ __forceinline__ void add_kept(float& sum, float x, const uint4& w, int i, unsigned thr) {
+    const unsigned h = i < 2 ? w.x : i < 4 ? w.y : i < 6 ? w.z : w.w;
+    asm("{\n\t.reg .pred p;\n\tsetp.ge.u32 p, %1, %2;\n\t@p add.f32 %0, %0, %3;\n\t}" : "+f"(sum) : "r"(i & 1 ? h : h << 16), "r"(thr), "f"(x));
+}
+
 // 8 elements as fp32.  WIDE: fp32 as one 256-bit access, else as two of 128 bits; bf16 is one of 128 either way.
 template <bool BF, bool WIDE>
 __device__ __forceinline__ Fv<8> load8(const void* base, long long e) {
@@ -88,20 +95,21 @@ __device__ __forceinline__ void store8_partial(void* base, long long e, const Fv
 // What a launch's item is: its tile, where it lies in `flat` and in the tensor.
 struct DropItem {
     long long flat0;     // first element in `flat`
-    long long elem0;     // ... in the tensor, a multiple of 8
-    long long nvalid;    // elements that exist in the tensor
+    long long block0;    // first run of 8 elements in the tensor
+    int nvalid;          // elements that exist in the tensor
     int nvec, seg;
     bool ok;
 };
 __device__ __forceinline__ DropItem item_of(const DropParams& P, long long item) {
     DropItem d;
-    const long long r = P.concat ? 0 : item / P.ntl;             // shard, counted from r0
+    // shard, counted from r0 (a division of 64 bits is a tenth of a tile's instructions)
+    const long long r = P.concat ? 0 : P.nitems <= 0xffffffffLL ? (long long)((unsigned)item / (unsigned)P.ntl) : item / P.ntl;
     const WsTile tl = P.tiles[P.tile_lo + (item - r * P.ntl)];
     const long long shard = P.concat ? tl.shard : P.r0 + r;
     d.flat0 = (shard - P.r0) * P.S + tl.pos;
-    d.elem0 = shard * tl.piece + tl.poff;
+    d.block0 = (shard * tl.piece + tl.poff) >> 3;
     const long long nv = tl.vt - shard * tl.piece;
-    d.nvalid = nv < 0 ? 0 : nv > tl.len ? (long long)tl.len : nv;
+    d.nvalid = nv < 0 ? 0 : nv > tl.len ? tl.len : (int)nv;
     d.nvec = tl.len >> 3;
     d.seg = tl.seg;
     d.ok = true;
@@ -113,10 +121,84 @@ __device__ __forceinline__ DropItem item_of(const DropParams& P, long long item)
 #endif
     return d;
 }
+__device__ __forceinline__ uint4 block_of(const DropParams& P, const DropItem& d, int i, unsigned now, int k) {
+    const long long j = d.block0 + i;
+    return philox(P, (unsigned)j, now, (unsigned)d.seg, P.replica + k + ((unsigned)(j >> 32) << 16));
+}
 
-// FBF, TBF: flat buffer, tensors in bf16.  SHORT: a warp per tile, else a CTA.
-template <bool FBF, bool TBF, bool WIDE, bool SHORT>
-__global__ void __launch_bounds__(256) hand_out_kernel(const __grid_constant__ DropParams P, const void* __restrict__ flat) {
+// 8 scaled elements as they are stored; `masked` of them: the dropped ones 0.
+template <bool TBF>
+struct Copy {
+    Fv<8> x;
+    __device__ __forceinline__ explicit Copy(const Fv<8>& v) : x(v) {}
+    __device__ __forceinline__ Copy masked(const uint4& w, unsigned thr) const {
+        Copy y(*this);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (!kept(w, e, thr)) y.x.f[e] = 0.f;
+        return y;
+    }
+    template <bool WIDE>
+    __device__ __forceinline__ void store(void* t, long long e) const { store8<false, WIDE>(t, e, x); }
+    __device__ __forceinline__ void store(void* t, long long e, int n) const { store_f32_partial<8>((float*)t + e, x, n); }
+};
+template <>
+struct Copy<true> {                // rounded once, whatever the number of sets
+    unsigned x[4];
+    __device__ __forceinline__ explicit Copy(const Fv<8>& v) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat162 b = __floats2bfloat162_rn(v.f[2 * i], v.f[2 * i + 1]);
+            x[i] = *reinterpret_cast<const unsigned*>(&b);
+        }
+    }
+    __device__ __forceinline__ Copy masked(const uint4& w, unsigned thr) const {
+        Copy y(*this);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (!kept(w, 2 * i, thr)) y.x[i] &= 0xffff0000u;
+            if (!kept(w, 2 * i + 1, thr)) y.x[i] &= 0x0000ffffu;
+        }
+        return y;
+    }
+    template <bool WIDE>
+    __device__ __forceinline__ void store(void* t, long long e) const {
+        __stcs(reinterpret_cast<uint4*>((unsigned short*)t + e), make_uint4(x[0], x[1], x[2], x[3]));
+    }
+    __device__ __forceinline__ void store(void* t, long long e, int n) const {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) ((unsigned short*)t)[e + i] = (unsigned short)(i & 1 ? x[i / 2] >> 16 : x[i / 2]);
+    }
+};
+
+// Hands U vectors, i, i + step, ..., out to every set; FULL: all their elements exist.
+template <bool FBF, bool TBF, bool WIDE, int U, bool FULL>
+__device__ __forceinline__ void hand_out(const DropParams& P, const DropItem& d, const void* flat, const void* const* sets, int i, int step, unsigned now) {
+    Fv<8> x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) x[u] = load8<FBF, WIDE>(flat, d.flat0 + 8LL * (i + u * step));
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[u].f[e] *= P.scale;
+#pragma unroll 1
+    for (int k = 0; k < P.nsets; ++k) {
+        void* t = const_cast<void*>(sets[k]);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int iu = i + u * step;
+            const Copy<TBF> y = Copy<TBF>(x[u]).masked(block_of(P, d, iu, now, k), P.thr);
+            if (FULL) y.template store<WIDE>(t, 8 * (d.block0 + iu));
+            else y.store(t, 8 * (d.block0 + iu), d.nvalid - 8 * iu);
+        }
+    }
+}
+
+// FBF, TBF: flat buffer, tensors in bf16.  SHORT: a warp per tile, else a CTA.  A thread holds U vectors of its tile, whose
+// loads are issued together, and writes them to one set after the other.
+template <bool FBF, bool TBF, bool WIDE, bool SHORT, int U, int MINB>
+__global__ void __launch_bounds__(256, MINB) hand_out_kernel(const __grid_constant__ DropParams P, const void* __restrict__ flat) {
     asm volatile("griddepcontrol.launch_dependents;");
     const int per_cta = SHORT ? blockDim.x >> 5 : 1;
     const int first = SHORT ? threadIdx.x & 31 : threadIdx.x, step = SHORT ? 32 : blockDim.x;
@@ -127,23 +209,13 @@ __global__ void __launch_bounds__(256) hand_out_kernel(const __grid_constant__ D
         asm volatile("griddepcontrol.wait;" ::: "memory");
         if (!d.ok) continue;
         const unsigned now = P.step + (P.step_dev ? *P.step_dev : 0u);
-        for (int i = first; i < d.nvec; i += step) {
-            const long long have = d.nvalid - 8LL * i;
-            if (have <= 0) break;
-            Fv<8> x = load8<FBF, WIDE>(flat, d.flat0 + 8LL * i);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x.f[e] *= P.scale;
-            const long long j = (d.elem0 >> 3) + i;
-            for (int k = 0; k < P.nsets; ++k) {
-                const uint4 w = philox(P, (unsigned)j, now, (unsigned)d.seg, P.replica + k + ((unsigned)(j >> 32) << 16));
-                Fv<8> y;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y.f[e] = kept(w, e, P.thr) ? x.f[e] : 0.f;
-                void* t = const_cast<void*>(sets[k]);
-                if (have >= 8) store8<TBF, WIDE>(t, 8 * j, y);
-                else store8_partial<TBF>(t, 8 * j, y, (int)have);
-            }
-        }
+        const int full = d.nvalid >> 3;
+        int i = first;
+        for (; i + (U - 1) * step < full; i += U * step) hand_out<FBF, TBF, WIDE, U, true>(P, d, flat, sets, i, step, now);
+        if (U > 1)
+#pragma unroll 1
+            for (; i < full; i += step) hand_out<FBF, TBF, WIDE, 1, true>(P, d, flat, sets, i, step, now);
+        if (8 * i < d.nvalid) hand_out<FBF, TBF, WIDE, 1, false>(P, d, flat, sets, i, step, now);       // the tensor's last elements
     }
 }
 
@@ -154,10 +226,70 @@ __device__ __forceinline__ void kahan_inf(float& s, float& c, float x) {
     s = t;
 }
 
-// The copies are summed in blocks of 4 whose loads are issued together; the blocks of more than 8 copies with compensation.
-constexpr int kSumBlock = 4;
-template <bool FBF, bool TBF, bool WIDE, bool SHORT>
-__global__ void __launch_bounds__(256) sum_kernel(const __grid_constant__ DropParams P, void* __restrict__ flat) {
+// Sums U vectors, i, i + step, ..., of all sets.  The copies are taken in blocks of KB whose loads are issued together;
+// COMP: more than 8 copies, whose blocks are added with compensation.
+template <bool FBF, bool TBF, bool WIDE, int KB, int U, bool COMP, bool FULL>
+__device__ __forceinline__ void sum_up(const DropParams& P, const DropItem& d, void* flat, const void* const* sets, int i, int step, unsigned now) {
+    Fv<8> sum[U], comp[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[u].f[e] = comp[u].f[e] = 0.f;
+#pragma unroll 1
+    for (int k0 = 0; k0 < P.nsets; k0 += KB) {
+        GradRaw<TBF, 8> raw[U][KB];
+#pragma unroll
+        for (int q = 0; q < KB; ++q) {
+            if (KB > 1 && k0 + q >= P.nsets) break;
+            const void* g = sets[k0 + q];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int iu = i + u * step;
+                if constexpr (!FULL) {
+                    raw[u][q] = load_grad_partial<TBF, 8>(g, 8 * (d.block0 + iu), d.nvalid - 8 * iu);
+                } else if constexpr (TBF) {
+                    raw[u][q] = load_grad<true, 8>(g, 8 * (d.block0 + iu));
+                } else {
+                    const Fv<8> v = load8<false, WIDE>(g, 8 * (d.block0 + iu));
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) raw[u][q].f[e] = v.f[e];
+                }
+            }
+        }
+        Fv<8> block[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) block[u].f[e] = COMP ? 0.f : sum[u].f[e];
+#pragma unroll
+        for (int q = 0; q < KB; ++q) {
+            if (KB > 1 && k0 + q >= P.nsets) break;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const uint4 w = block_of(P, d, i + u * step, now, k0 + q);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) add_kept(block[u].f[e], raw_elem<TBF, 8>(raw[u][q], e), w, e, P.thr);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                if (COMP) kahan_inf(sum[u].f[e], comp[u].f[e], block[u].f[e]);
+                else sum[u].f[e] = block[u].f[e];
+            }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int iu = i + u * step, have = d.nvalid - 8 * iu;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[u].f[e] = FULL || e < have ? sum[u].f[e] * P.scale : 0.f;
+        store8<FBF, WIDE>(flat, d.flat0 + 8LL * iu, sum[u]);
+    }
+}
+
+template <bool FBF, bool TBF, bool WIDE, bool SHORT, int KB, int U, bool COMP, int MINB>
+__global__ void __launch_bounds__(256, MINB) sum_kernel(const __grid_constant__ DropParams P, void* __restrict__ flat) {
     asm volatile("griddepcontrol.launch_dependents;");
     const int per_cta = SHORT ? blockDim.x >> 5 : 1;
     const int first = SHORT ? threadIdx.x & 31 : threadIdx.x, step = SHORT ? 32 : blockDim.x;
@@ -167,49 +299,17 @@ __global__ void __launch_bounds__(256) sum_kernel(const __grid_constant__ DropPa
         asm volatile("griddepcontrol.wait;" ::: "memory");
         if (!d.ok) continue;
         const unsigned now = P.step + (P.step_dev ? *P.step_dev : 0u);
-        for (int i = first; i < d.nvec; i += step) {
-            const long long have = d.nvalid - 8LL * i;
-            const long long j = (d.elem0 >> 3) + i;
-            Fv<8> sum, comp;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum.f[e] = comp.f[e] = 0.f;
-            for (int k0 = 0; have > 0 && k0 < P.nsets; k0 += kSumBlock) {
-                GradRaw<TBF, 8> raw[kSumBlock];
-#pragma unroll
-                for (int q = 0; q < kSumBlock; ++q) {
-                    const int k = k0 + q < P.nsets ? k0 + q : k0;
-                    if (have >= 8) {
-                        if constexpr (TBF) {
-                            raw[q] = load_grad<true, 8>(sets[k], 8 * j);
-                        } else {
-                            const Fv<8> v = load8<false, WIDE>(sets[k], 8 * j);
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) raw[q].f[e] = v.f[e];
-                        }
-                    } else {
-                        raw[q] = load_grad_partial<TBF, 8>(sets[k], 8 * j, (int)have);
-                    }
-                }
-                Fv<8> block;
-#pragma unroll
-                for (int q = 0; q < kSumBlock; ++q) {
-                    const uint4 w = philox(P, (unsigned)j, now, (unsigned)d.seg, P.replica + k0 + q + ((unsigned)(j >> 32) << 16));
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float v = k0 + q < P.nsets && kept(w, e, P.thr) ? raw_elem<TBF, 8>(raw[q], e) : 0.f;
-                        block.f[e] = q == 0 ? v : block.f[e] + v;
-                    }
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    if (P.nsets > 8) kahan_inf(sum.f[e], comp.f[e], block.f[e]);
-                    else sum.f[e] += block.f[e];
-                }
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum.f[e] = e < have ? sum.f[e] * P.scale : 0.f;
-            store8<FBF, WIDE>(flat, d.flat0 + 8LL * i, sum);
+        const int full = d.nvalid >> 3;
+        int i = first;
+        for (; i + (U - 1) * step < full; i += U * step) sum_up<FBF, TBF, WIDE, KB, U, COMP, true>(P, d, flat, sets, i, step, now);
+        if (U > 1)
+#pragma unroll 1
+            for (; i < full; i += step) sum_up<FBF, TBF, WIDE, KB, 1, COMP, true>(P, d, flat, sets, i, step, now);
+        if (8 * i < d.nvalid) {          // the tensor's last elements
+            sum_up<FBF, TBF, WIDE, 1, 1, COMP, false>(P, d, flat, sets, i, step, now);
+            i += step;
         }
+        for (; i < d.nvec; i += step) store8<FBF, WIDE>(flat, d.flat0 + 8LL * i, Fv<8>{});             // padding
     }
 }
 
@@ -227,18 +327,54 @@ void launch(void (*kernel)(KArgs...), long long grid, int block, cudaStream_t st
     cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
 }
 
+// How a call's tiles are cut up: tiles, elements of the plan's tile, a warp per tile or a CTA.
+struct Shape {
+    long long items;
+    int tile;
+    bool is_short;
+};
+// CTAs of `most` threads, fewer where a tile would not give each of them `unroll` vectors.
+template <typename Kernel, typename Flat>
+void launch_tiles(Kernel kernel, const Shape& s, int most, int unroll, cudaStream_t st, const DropParams& P, Flat flat) {
+    int threads = s.is_short ? 128 : most;
+    while (!s.is_short && threads > 32 && s.tile / 8 < unroll * threads) threads >>= 1;
+    const int per_cta = s.is_short ? threads / 32 : 1;
+    const long long grid = (s.items + per_cta - 1) / per_cta;
+    launch(kernel, grid < 0x7fffffffLL ? grid : 0x7fffffffLL, threads, st, P, flat);
+}
+
+// Drawing the masks is what these kernels do beside the copy: 14 products of 32 x 32 bits and as many three-way exclusive ors
+// per block of 8 elements and set, and a comparison and a choice per element.  On bf16 tensors that is 10 instructions an
+// element, half of them of the integer pipe's half rate, near what the copy leaves time for; fp32 tensors have twice the time.
+// So small CTAs (a long tile's latencies overlap with other tiles'), registers for many of them, no more loads in flight than
+// that needs.  us by threads of a CTA, 335 M elements from bf16 to one bf16 list: 256 249, 128 225, 64 213 (205 at the copy
+// bandwidth); the sum of one bf16 list 260 / 237 / 228, of 2 of 61 M 89 / 89 / 79 (75), of 4 of 1.56 G 2916 / 2920 / 2972
+// (2859); 4 bf16 lists from an fp32 state of 451 M 899 / 857 / 887 (828).  With 3 CTAs of 256 instead of 6 the sum
+// of 4 lists takes 3275.  More than 8 bf16 lists: blocks of 8 halve the compensation's steps, 16 lists of 61 M 460 -> 399 (338).
 template <bool FBF, bool TBF, bool WIDE, bool SHORT>
-void launch_op(bool sum, void* flat, long long grid, int threads, cudaStream_t st, const DropParams& P) {
-    if (sum) launch(sum_kernel<FBF, TBF, WIDE, SHORT>, grid, threads, st, P, flat);
-    else launch(hand_out_kernel<FBF, TBF, WIDE, SHORT>, grid, threads, st, P, (const void*)flat);
+void launch_op(bool sum, void* flat, const Shape& s, cudaStream_t st, const DropParams& P) {
+    const void* from = flat;
+    if (!sum) {
+        if (FBF && TBF) launch_tiles(hand_out_kernel<FBF, TBF, WIDE, SHORT, 4, 5>, s, 64, 4, st, P, from);
+        else if (P.nsets == 1) launch_tiles(hand_out_kernel<FBF, TBF, WIDE, SHORT, 2, 3>, s, 64, 2, st, P, from);
+        else launch_tiles(hand_out_kernel<FBF, TBF, WIDE, SHORT, 2, 1>, s, 128, 2, st, P, from);
+    } else if (P.nsets == 1) {
+        launch_tiles(sum_kernel<FBF, TBF, WIDE, SHORT, 1, 2, false, TBF ? 5 : 4>, s, 64, 2, st, P, flat);
+    } else if (P.nsets == 2) {
+        launch_tiles(sum_kernel<FBF, TBF, WIDE, SHORT, 2, TBF ? 2 : 1, false, 4>, s, 64, TBF ? 2 : 1, st, P, flat);
+    } else if (P.nsets <= 8) {
+        launch_tiles(sum_kernel<FBF, TBF, WIDE, SHORT, 4, 1, false, TBF ? 6 : 3>, s, 128, 1, st, P, flat);
+    } else {
+        launch_tiles(sum_kernel<FBF, TBF, WIDE, SHORT, TBF ? 8 : 4, 1, true, TBF ? 3 : 4>, s, TBF ? 64 : 128, 1, st, P, flat);
+    }
 }
 template <bool FBF, bool TBF>
-void launch_types(bool sum, bool wide, bool is_short, void* flat, long long grid, int threads, cudaStream_t st, const DropParams& P) {
+void launch_types(bool sum, bool wide, void* flat, const Shape& s, cudaStream_t st, const DropParams& P) {
     if constexpr (FBF && TBF) {         // no fp32 access: WIDE says nothing
-        (is_short ? launch_op<FBF, TBF, true, true> : launch_op<FBF, TBF, true, false>)(sum, flat, grid, threads, st, P);
+        (s.is_short ? launch_op<FBF, TBF, true, true> : launch_op<FBF, TBF, true, false>)(sum, flat, s, st, P);
     } else {
-        if (wide) (is_short ? launch_op<FBF, TBF, true, true> : launch_op<FBF, TBF, true, false>)(sum, flat, grid, threads, st, P);
-        else (is_short ? launch_op<FBF, TBF, false, true> : launch_op<FBF, TBF, false, false>)(sum, flat, grid, threads, st, P);
+        if (wide) (s.is_short ? launch_op<FBF, TBF, true, true> : launch_op<FBF, TBF, true, false>)(sum, flat, s, st, P);
+        else (s.is_short ? launch_op<FBF, TBF, false, true> : launch_op<FBF, TBF, false, false>)(sum, flat, s, st, P);
     }
 }
 
@@ -285,15 +421,10 @@ ws_status run(bool sum, const ws_plan* p, int32_t r, void* flat, ws_dtype flat_d
     const bool wide = table->min_align >= 32 && (reinterpret_cast<uintptr_t>(flat) & 31u) == 0;
     // a warp per tile where tiles are short (ws_pack's rule, in elements of the wider type)
     const long long tile = p->ntiles > 0 ? (P.concat ? p->S * p->R : p->S) / p->ntiles : p->K;
-    const bool is_short = P.nitems > 32LL * p->sms && tile <= 768 && p->longest <= 128 << 10;
-    int threads = is_short ? 128 : 256;
-    while (!is_short && threads > 64 && p->K / 8 < 2 * threads) threads >>= 1;
-    const int per_cta = is_short ? threads / 32 : 1;
-    long long grid = (P.nitems + per_cta - 1) / per_cta;
-    if (grid > 0x7fffffffLL) grid = 0x7fffffffLL;
+    const Shape s{P.nitems, p->K, P.nitems > 32LL * p->sms && tile <= 768 && p->longest <= 128 << 10};
     cudaStream_t st = (cudaStream_t)stream;
-    if (flat_dtype == WS_BF16) (table->dtype == WS_BF16 ? launch_types<true, true> : launch_types<true, false>)(sum, wide, is_short, flat, grid, threads, st, P);
-    else (table->dtype == WS_BF16 ? launch_types<false, true> : launch_types<false, false>)(sum, wide, is_short, flat, grid, threads, st, P);
+    if (flat_dtype == WS_BF16) (table->dtype == WS_BF16 ? launch_types<true, true> : launch_types<true, false>)(sum, wide, flat, s, st, P);
+    else (table->dtype == WS_BF16 ? launch_types<false, true> : launch_types<false, false>)(sum, wide, flat, s, st, P);
     return ws_check_launch(sum ? "ws_reduce_dropout" : "ws_unpack_dropout");
 }
 
