@@ -647,7 +647,7 @@ ws_status ws_reduce_dropout(const ws_plan* plan, int32_t r, const ws_tensor_tabl
  *             contiguous.  A number outside 0 ... experts - 1 is no pick (a token that a full expert
  *             refused); one that stands in a row twice counts twice
  *   valid     NULL, or [replicas] device pointers (or NULL) to [tokens] bytes: a token with byte 0 does not
- *             exist (the end of a padded sequence): its picks do not count, its logits are not read (they may hold
+ *             exist (the end of a padded sequence): its picks do not count, its logits enter nothing (they may hold
  *             NaN) and their gradient is 0
  *   logits    [layers][replicas] device pointers to [tokens] rows of `experts` elements of `dtype`, row n at
  *             n * logits_ld (>= experts) elements
