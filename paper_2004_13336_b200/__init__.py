@@ -13,6 +13,11 @@ of the C functions::
     ws.ws_fused_update(plan, -1, ws.TensorTable(plan, grad_lists), w, m, v, hyper,
                        ws.TensorTable(plan, [weight_tensors]))   # the same step in one kernel
 
+    ws.ws_unpack_dropout(plan, -1, w, tables, ws.make_dropout(p, seed, step))     # each replica its own random part
+    ws.ws_reduce_dropout(plan, -1, grad_tables, drop, summed)         # ... and their gradients' sum, one copy for the update
+    ws.ws_router_counts(routers, counts)                              # balance of a model's experts over all replicas
+    ws.ws_balance_loss(routers, counts, loss, coef, workspace=scratch)
+
 ``workloads.py`` holds the model-shaped synthetic tensor sets used by the
 tests and the benchmark.  There is no CPU fallback: without the built library
 every call fails at import of the binding.

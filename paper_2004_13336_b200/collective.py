@@ -15,12 +15,14 @@ own input and output layout, so no extra copy sits between a collective and a ke
 
 ``ops`` names the module that supplies ``Plan``, ``ws_pack``, ``ws_unpack``,
 ``ws_shard_update``, ``ws_lamb_partial / _finalize / _apply``, ``ws_lars_partial / _finalize /
-_apply``, ``ws_adafactor_stage``, ``lamb_partials``, ``adafactor_sums`` and ``make_hyper``; it is the CUDA binding unless a test passes a
+_apply``, ``ws_adafactor_stage``, ``lamb_partials``, ``adafactor_sums`` and ``make_hyper`` (with dropout also
+``TensorTable``, ``make_dropout``, ``ws_unpack_dropout`` and ``ws_reduce_dropout``; for ``ExpertBalance``
+``ws_router_counts`` and ``ws_balance_loss``); it is the CUDA binding unless a test passes a
 stand-in to run the choreography on CPU ranks.
 """
 from __future__ import annotations
 
-from typing import Dict, Optional, Sequence
+from typing import Dict, Optional, Sequence, Tuple
 
 import torch
 import torch.distributed as dist
@@ -32,7 +34,10 @@ class ShardedUpdate:
 
     def __init__(self, shapes: Sequence[Sequence[int]], opt: str, hyper: Dict[str, float],
                  out_dtype: torch.dtype = torch.float32, grad_dtype: torch.dtype = torch.float32,
-                 align_elems: int = 32, device=None, group=None, ops=None):
+                 align_elems: int = 32, device=None, group=None, ops=None,
+                 dropout: Optional[Tuple[float, int]] = None):
+        """``dropout``: (p, seed).  Every replica then trains on its own random part of the weights: ``hand_out`` gives
+        it the first step's, each ``step`` takes the gradients of the present part and hands the next one out."""
         if ops is None:
             from . import binding as ops      # fails loudly without the built CUDA library
         if opt not in ("sgdm", "adam", "lamb", "lars", "adafactor"):
@@ -51,6 +56,7 @@ class ShardedUpdate:
         if opt in ("lamb", "lars", "adafactor"):
             self.workspace = torch.zeros(max(16, self.plan.workspace_bytes(opt)), dtype=torch.uint8,
                                          device=self.device)
+        self.dropout, self.drawn = dropout, 0             # masks handed out last: those of step `drawn`
         self.fstate = None                                                    # Adafactor: replicated, small
         if opt == "adafactor":
             self.fstate = torch.zeros(self.plan.factored_elems, **z)
@@ -69,15 +75,35 @@ class ShardedUpdate:
         dist.all_gather_into_tensor(full, shard, group=self.group)
         self.ops.ws_unpack(self.plan, full, out)
 
+    # -- weight dropout ----------------------------------------------------------------------
+    def _table(self, tensors):
+        return tensors if isinstance(tensors, self.ops.TensorTable) else self.ops.TensorTable(self.plan, [list(tensors)])
+
+    def _masks(self, step: int):
+        p, seed = self.dropout
+        return self.ops.make_dropout(p, seed, step, self.rank)
+
+    def hand_out(self, weights_out):
+        """Gathers the present weights and hands this replica's part of them out, under the masks that the next
+        ``step``'s gradients belong to (with ``dropout`` only; ``self.drawn`` counts the steps)."""
+        S, r = self.plan.S, self.rank
+        self.gathered[r * S:(r + 1) * S].copy_(self.w)
+        dist.all_gather_into_tensor(self.gathered, self.gathered[r * S:(r + 1) * S], group=self.group)
+        self.ops.ws_unpack_dropout(self.plan, -1, self.gathered, self._table(weights_out), self._masks(self.drawn))
+
     def step(self, grads: Sequence[torch.Tensor], weights_out: Sequence[torch.Tensor], step: Optional[int] = None):
         """One training step's weight update.  ``grads``: this replica's local gradients, one tensor
         per model tensor.  ``weights_out``: the model's weight tensors (``out_dtype``), overwritten
-        with the updated full weights."""
+        with the updated full weights (with ``dropout``: this replica's next part of them; both may then be
+        tables made once, ``ops.TensorTable(su.plan, [tensors])``, and are where the step is captured)."""
         ops, plan, r, S = self.ops, self.plan, self.rank, self.plan.S
         if step is not None:
             self.hyper_dict["step"] = step
         hy = ops.make_hyper(self.opt, self.hyper_dict)
-        ops.ws_pack(plan, grads, self.packed)                                   # formatting (Section 5.1)
+        if self.dropout is None:
+            ops.ws_pack(plan, grads, self.packed)                               # formatting (Section 5.1)
+        else:                                                                   # ... under this replica's masks
+            ops.ws_reduce_dropout(plan, -1, self._table(grads), self._masks(self.drawn), self.packed)
         dist.reduce_scatter_tensor(self.recv, self.packed, op=dist.ReduceOp.SUM, group=self.group)
         if self.opt == "lamb":
             ops.ws_lamb_partial(plan, r, [self.recv], self.w, self.m, self.v, hy, self.workspace, slice_mode=1)
@@ -109,7 +135,38 @@ class ShardedUpdate:
             ops.ws_shard_update(plan, r, [self.recv], self.w, self.m, self.v if self.opt == "adam" else None,
                                 hy, self.gathered, None, slice_mode=1)
         dist.all_gather_into_tensor(self.gathered, self.gathered[r * S:(r + 1) * S], group=self.group)
-        ops.ws_unpack(plan, self.gathered, weights_out)                         # reverse formatting
+        if self.dropout is None:
+            ops.ws_unpack(plan, self.gathered, weights_out)                     # reverse formatting
+        else:
+            self.drawn += 1
+            ops.ws_unpack_dropout(plan, -1, self.gathered, self._table(weights_out), self._masks(self.drawn))
+
+
+class ExpertBalance:
+    """The load-balancing loss of a mixture-of-experts model over all replicas' tokens.  The counts of the experts'
+    picks are sums over the replicas (one all-reduce for all layers); with them every replica forms its own part of
+    the losses and its own logits' gradient in one pass, and the losses' parts are summed again."""
+
+    def __init__(self, layers: int, experts: int, coef: float, z_coef: float = 0.0, device=None, group=None, ops=None):
+        if ops is None:
+            from . import binding as ops
+        self.ops, self.coef, self.z_coef, self.group = ops, coef, z_coef, group
+        device = torch.device(device) if device is not None else torch.device("cuda", torch.cuda.current_device())
+        self.counts = torch.zeros(layers, experts + 1, dtype=torch.int64, device=device)
+        self.loss = torch.zeros(layers, 2, device=device)
+        self.workspace = None
+
+    def step(self, routers, upstream: Optional[torch.Tensor] = None, accumulate: bool = False) -> torch.Tensor:
+        """``routers``: this replica's tensors (``ops.RouterSet``, with one replica's lists).  Fills their dlogits and
+        returns the batch's losses [layers][2]; ``self.counts`` holds the batch's counts, the tokens' number last."""
+        need = routers.workspace_bytes()
+        if self.workspace is None or self.workspace.numel() < need:
+            self.workspace = torch.empty(max(16, need), dtype=torch.uint8, device=self.counts.device)
+        self.ops.ws_router_counts(routers, self.counts)
+        dist.all_reduce(self.counts, group=self.group)
+        self.ops.ws_balance_loss(routers, self.counts, self.loss, self.coef, self.z_coef, upstream, accumulate, self.workspace)
+        dist.all_reduce(self.loss, group=self.group)
+        return self.loss
 
 
 class PeerShardedUpdate:
