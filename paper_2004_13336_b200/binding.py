@@ -719,15 +719,19 @@ def make_dropout(p: float, seed: int, step: int = 0, replica: int = 0,
     if step_dev is not None:
         if step_dev.dtype not in (torch.int32, torch.uint32) or step_dev.numel() != 1 or not step_dev.is_cuda:
             raise TypeError("step_dev is a device tensor of one 32-bit integer")
-    d = ws_dropout(float(p), int(seed) & 0xFFFFFFFFFFFFFFFF, int(step) & 0xFFFFFFFF, int(replica),
-                   step_dev.data_ptr() if step_dev is not None else None)
-    d._keep = step_dev
-    return d
+        d = ws_dropout(p, int(seed) & 0xFFFFFFFFFFFFFFFF, int(step) & 0xFFFFFFFF, replica, step_dev.data_ptr())
+        d._keep = step_dev
+        return d
+    return ws_dropout(p, int(seed) & 0xFFFFFFFFFFFFFFFF, int(step) & 0xFFFFFFFF, replica)
+
+
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)      # (without the Python around it)
 
 
 def _on_current_device(t):
     """The calls launch on the current device's current stream: a tensor of another device has no place there."""
-    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+    d = t.get_device()
+    if d < 0 or d != _current_device():
         raise ValueError(f"a tensor on the current device expected, not on {t.device}")
 
 
@@ -829,6 +833,8 @@ class RouterSet:
                 arr[k] = t.data_ptr()
             keep.extend((list(valid), arr))
             c.valid = C.cast(arr, C.POINTER(C.c_void_p))
+        self._index = self.device.index if self.device.type == "cuda" else -1
+        self._counts_shape, self._loss_shape = (layers, self.experts + 1), (layers, 2)
         self._tokens = (C.c_int64 * replicas)(*tokens)
         c.tokens = C.cast(self._tokens, C.POINTER(C.c_int64))
         self.addr = C.addressof(c)
@@ -839,10 +845,10 @@ class RouterSet:
 
 
 def _router_addr(routers, counts):
-    if not isinstance(routers, RouterSet):
+    if type(routers) is not RouterSet and not isinstance(routers, RouterSet):
         raise TypeError(f"expected RouterSet instead of {type(routers).__name__}")
-    if (counts.dtype != torch.int64 or tuple(counts.shape) != (routers.layers, routers.experts + 1) or not counts.is_contiguous()
-            or counts.device != routers.device):
+    if (counts.dtype is not torch.int64 or counts.shape != routers._counts_shape or not counts.is_contiguous()
+            or counts.get_device() != routers._index):
         raise ValueError(f"counts: a contiguous int64 tensor [{routers.layers}, {routers.experts + 1}] beside the routers' tensors")
     _on_current_device(counts)
     return routers.addr
@@ -862,10 +868,13 @@ def ws_balance_loss(routers: RouterSet, counts: torch.Tensor, loss: Optional[tor
     """The load-balancing loss and the z loss of every layer (loss[l][0], loss[l][1]) and, into the set's dlogits, the
     gradient of ``upstream`` (a device float, else 1) times their sum by the logits."""
     addr = _router_addr(routers, counts)
-    if loss is not None and (loss.dtype != torch.float32 or tuple(loss.shape) != (routers.layers, 2) or not loss.is_contiguous()):
-        raise ValueError(f"loss: a contiguous float32 tensor [{routers.layers}, 2]")
-    if upstream is not None and (upstream.dtype != torch.float32 or upstream.numel() != 1 or not upstream.is_cuda):
-        raise TypeError("upstream: a device tensor of one float32")
+    if loss is not None and (loss.dtype is not torch.float32 or loss.shape != routers._loss_shape or not loss.is_contiguous()
+                             or loss.get_device() != routers._index):
+        raise ValueError(f"loss: a contiguous float32 tensor [{routers.layers}, 2] beside the routers' tensors")
+    if upstream is not None and (upstream.dtype is not torch.float32 or upstream.numel() != 1 or upstream.get_device() != routers._index):
+        raise TypeError("upstream: a tensor of one float32 beside the routers' tensors")
+    if workspace is not None and workspace.get_device() != routers._index:
+        raise ValueError("workspace: a tensor beside the routers' tensors")
     st = _step().ws_balance_loss(addr, counts.data_ptr(), loss.data_ptr() if loss is not None else None, coef, z_coef,
                                  upstream.data_ptr() if upstream is not None else None, 1 if accumulate else 0,
                                  workspace.data_ptr() if workspace is not None else None,
