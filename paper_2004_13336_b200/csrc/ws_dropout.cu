@@ -419,9 +419,11 @@ ws_status run(bool sum, const ws_plan* p, int32_t r, void* flat, ws_dtype flat_d
     P.flat_elems = (r < 0 ? (long long)p->R : 1) * p->S;
 #endif
     const bool wide = table->min_align >= 32 && (reinterpret_cast<uintptr_t>(flat) & 31u) == 0;
-    // a warp per tile where tiles are short (ws_pack's rule, in elements of the wider type)
+    // A warp per tile where tiles are short and many, and not long enough in any place to leave a warp walking alone (ws_pack's
+    // rule, in elements).  us, a CTA / a warp per tile: 64 shards of 47 M in tiles of 900, sum of one bf16 list 56 / 40, fp32 to one
+    // list 61 / 60; 16 bf16 lists of 4 M in tiles of 660, whose draws are enough work for a CTA, 38 / 50.
     const long long tile = p->ntiles > 0 ? (P.concat ? p->S * p->R : p->S) / p->ntiles : p->K;
-    const Shape s{P.nitems, p->K, P.nitems > 32LL * p->sms && tile <= 768 && p->longest <= 128 << 10};
+    const Shape s{P.nitems, p->K, P.nitems > 32LL * p->sms && tile <= (P.nsets <= 2 ? 1024 : P.nsets <= 8 ? 768 : 0) && p->longest <= 128 << 10};
     cudaStream_t st = (cudaStream_t)stream;
     if (flat_dtype == WS_BF16) (table->dtype == WS_BF16 ? launch_types<true, true> : launch_types<true, false>)(sum, wide, flat, s, st, P);
     else (table->dtype == WS_BF16 ? launch_types<false, true> : launch_types<false, false>)(sum, wide, flat, s, st, P);

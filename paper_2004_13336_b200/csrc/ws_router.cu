@@ -688,13 +688,13 @@ Deal launch_score(const ws_router_set* s, const BalanceParams& P, const RouterTa
 }
 // A lane holds up to 16 elements of a row in vectors (fewer shuffles, and less of what every lane does once a row), up to 8 single
 // ones (rows off the 16-byte boundaries: bf16 rows of 60, 15.7 M, 41 us, with 2 elements 77, with 16 40; fp32 rows of 33 29, 55, 30),
-// more where 32 lanes do not hold the row that way.
+// more where 32 lanes do not hold the row that way.  Short fp32 rows keep two lanes side by side (rows of 16 20 -> 17; bf16 16 -> 19).
 template <typename X, int NP, int NR>
 Deal launch_shape(const ws_router_set* s, bool wide, BalanceParams& P, const RouterTab<NP, NR>& tab, cudaStream_t st) {
     constexpr int V = 16 / sizeof(X);
     const int vecs = wide ? s->experts / V : s->experts;
     int c = 1;
-    while (2 * c * (wide ? V : 1) <= (wide ? 16 : 8) && 2 * c <= vecs) c *= 2;
+    while (2 * c * (wide ? V : 1) <= (wide ? 16 : 8) && (wide && V == 4 && vecs > 2 ? 4 : 2) * c <= vecs) c *= 2;
     while ((vecs + c - 1) / c > 32) c *= 2;
     P.lanes = 1;
     while (P.lanes * c < vecs) P.lanes *= 2;
