@@ -651,7 +651,8 @@ ws_status ws_reduce_dropout(const ws_plan* plan, int32_t r, const ws_tensor_tabl
  *             NaN) and their gradient is 0
  *   logits    [layers][replicas] device pointers to [tokens] rows of `experts` elements of `dtype`, row n at
  *             n * logits_ld (>= experts) elements
- *   dlogits   the gradients' rows, likewise with dlogits_ld; NULL for the loss alone.  May be the logits.
+ *   dlogits   the gradients' rows, likewise with dlogits_ld, distinct memory; NULL for the loss alone.  May be the
+ *             logits themselves, tensor by tensor at the same stride.
  * Pointers are aligned to their elements; rows on 16-byte boundaries take the vectors' path.  A pointer of a
  * replica without tokens is not read and may be NULL; so may picks in ws_balance_loss and logits and dlogits in
  * ws_router_counts.
@@ -667,7 +668,8 @@ ws_status ws_reduce_dropout(const ws_plan* plan, int32_t r, const ws_tensor_tabl
  *   upstream      device float u, or NULL for 1
  *   workspace     device scratch of ws_balance_workspace_bytes(set) bytes, 16-byte aligned; nothing in it
  *                 has to be cleared.  Calls that can run at the same time need one each.
- * Sums over tokens are formed in 64 bits in a fixed order: the same call gives the same bits. */
+ * Sums over tokens are formed in 64 bits in a fixed order: the same call gives the same bits.
+ * More than 2^34 tokens in a layer may be refused with WS_ERR_TOO_LARGE. */
 typedef enum { WS_SOFTMAX = 0, WS_SIGMOID = 1 } ws_score;
 typedef struct {
     int32_t layers, replicas, experts, topk;

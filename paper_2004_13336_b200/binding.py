@@ -719,10 +719,10 @@ def make_dropout(p: float, seed: int, step: int = 0, replica: int = 0,
     if step_dev is not None:
         if step_dev.dtype not in (torch.int32, torch.uint32) or step_dev.numel() != 1 or not step_dev.is_cuda:
             raise TypeError("step_dev is a device tensor of one 32-bit integer")
-        d = ws_dropout(p, int(seed) & 0xFFFFFFFFFFFFFFFF, int(step) & 0xFFFFFFFF, replica, step_dev.data_ptr())
+        d = ws_dropout(float(p), int(seed) & 0xFFFFFFFFFFFFFFFF, int(step) & 0xFFFFFFFF, int(replica), step_dev.data_ptr())
         d._keep = step_dev
         return d
-    return ws_dropout(p, int(seed) & 0xFFFFFFFFFFFFFFFF, int(step) & 0xFFFFFFFF, replica)
+    return ws_dropout(float(p), int(seed) & 0xFFFFFFFFFFFFFFFF, int(step) & 0xFFFFFFFF, int(replica))
 
 
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)      # (without the Python around it)

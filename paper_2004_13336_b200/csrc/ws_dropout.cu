@@ -215,7 +215,7 @@ __global__ void __launch_bounds__(256, MINB) hand_out_kernel(const __grid_consta
         if (U > 1)
 #pragma unroll 1
             for (; i < full; i += step) hand_out<FBF, TBF, WIDE, 1, true>(P, d, flat, sets, i, step, now);
-        if (8 * i < d.nvalid) hand_out<FBF, TBF, WIDE, 1, false>(P, d, flat, sets, i, step, now);       // the tensor's last elements
+        if (i == full && (d.nvalid & 7)) hand_out<FBF, TBF, WIDE, 1, false>(P, d, flat, sets, i, step, now);       // the tensor's last elements
     }
 }
 
@@ -305,7 +305,7 @@ __global__ void __launch_bounds__(256, MINB) sum_kernel(const __grid_constant__ 
         if (U > 1)
 #pragma unroll 1
             for (; i < full; i += step) sum_up<FBF, TBF, WIDE, KB, 1, COMP, true>(P, d, flat, sets, i, step, now);
-        if (8 * i < d.nvalid) {          // the tensor's last elements
+        if (i == full && (d.nvalid & 7)) {          // the tensor's last elements
             sum_up<FBF, TBF, WIDE, 1, 1, COMP, false>(P, d, flat, sets, i, step, now);
             i += step;
         }

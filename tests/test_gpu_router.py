@@ -252,6 +252,45 @@ def test_same_call_same_bits_and_captured():
         assert all(torch.equal(a, b) for a, b in zip(first, (t for layer in dlogits for t in layer)))
 
 
+def test_two_streams_at_once():
+    """Two sets, each with its own counts and workspace, against the same calls one after the other."""
+    sets = []
+    for seed in (1, 2):
+        picks, logits, dlogits, valid, _ = make(6, [9000, 5000], 64, 2, seed=seed, valid=0.9)
+        routers = B.RouterSet(64, picks, valid, logits, dlogits)
+        sets.append((routers, torch.empty(6, 65, dtype=torch.int64, device=DEV), torch.empty(6, 2, device=DEV),
+                     torch.empty(routers.workspace_bytes(), dtype=torch.uint8, device=DEV), dlogits))
+
+    def call(routers, counts, loss, ws, dlogits):
+        B.ws_router_counts(routers, counts)
+        B.ws_balance_loss(routers, counts, loss, 1e-2, 1e-3, workspace=ws)
+
+    want = []
+    for s in sets:
+        call(*s)
+        want.append([s[1].clone(), s[2].clone()] + [t.clone() for layer in s[4] for t in layer])
+    for s in sets:
+        for t in (s[1], s[2], *(t for layer in s[4] for t in layer)):
+            t.zero_()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    for _ in range(5):
+        for s, stream in zip(sets, streams):
+            with torch.cuda.stream(stream):
+                call(*s)
+    torch.cuda.synchronize()
+    for s, w in zip(sets, want):
+        assert all(torch.equal(a, b) for a, b in zip([s[1], s[2]] + [t for layer in s[4] for t in layer], w))
+
+
+def test_many_small_replicas_and_layers_of_one_call():
+    """More (layer, replica) pairs than a launch takes, replicas that share a CTA, one that has nothing."""
+    tokens = [3, 0, 1, 7, 2, 11, 0, 5, 4, 1, 1, 6, 9, 2, 8, 3, 2]
+    for dtype, score in ((F32, "softmax"), (BF16, "sigmoid")):
+        picks, logits, dlogits, valid, _ = make(40, tokens, 24, 3, dtype, torch.int32, valid=0.8)
+        check(picks, logits, dlogits, valid, 24, 3, score, z=1e-2 if score == "softmax" else 0.0)
+
+
 def test_gradient_follows_differences_of_the_loss():
     """Steps of 2^-6 along single logits: (L(x + h) - L(x - h)) / 2h against the gradient.  L is a float32 (2^-24 of it), its
     third derivative at most 6 L per logit, so the difference is off by h^2 L + 2^-24 L / h < 2^-11 L at most."""

@@ -121,6 +121,13 @@ def test_dropout_refuses_bad_arguments(uploaded, name):
         assert call(**ok) == NOT_UPLOADED
 
 
+def test_make_dropout_takes_numbers_of_any_kind():
+    d = B.make_dropout(np.float32(0.5), np.int64(3), np.int32(4), np.int64(5))
+    assert (d.p, d.seed, d.step, d.replica, d.step_dev) == (0.5, 3, 4, 5, None)
+    d = B.make_dropout(0, -1, -1)
+    assert (d.p, d.seed, d.step, d.replica) == (0.0, 2 ** 64 - 1, 2 ** 32 - 1, 0)
+
+
 def test_dropout_binding_refuses_what_is_no_buffer_of_its_size(uploaded, monkeypatch):
     monkeypatch.setattr(B, "_on_current_device", lambda t: None)
     lists = type("T", (), {"c": _table(2)})()
