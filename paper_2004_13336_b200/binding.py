@@ -728,20 +728,26 @@ def make_dropout(p: float, seed: int, step: int = 0, replica: int = 0,
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)      # (without the Python around it)
 
 
-def _on_current_device(t):
-    """The calls launch on the current device's current stream: a tensor of another device has no place there."""
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
+def _on_current_device(t) -> int:
+    """The calls launch on the current device's current stream: a tensor of another device has no place there.  Returns
+    the device."""
     d = t.get_device()
     if d < 0 or d != _current_device():
         raise ValueError(f"a tensor on the current device expected, not on {t.device}")
+    return d
 
 
 def _check_flat(plan, r, flat):
     """ws_unpack_dropout and ws_reduce_dropout take a whole layout or one shard by ``r``: its size is all that tells a
     buffer of the other kind from the right one."""
-    _on_current_device(flat)
+    device = _on_current_device(flat)
     want = plan.G if r < 0 else plan.S
     if flat.numel() != want or not flat.is_contiguous():
         raise ValueError(f"flat is a contiguous buffer of {want} elements for r = {r}, not {tuple(flat.shape)}")
+    return device
 
 
 def ws_unpack_dropout(plan: Plan, r: int, flat: torch.Tensor, lists: TensorTable, drop: ws_dropout):
@@ -749,9 +755,9 @@ def ws_unpack_dropout(plan: Plan, r: int, flat: torch.Tensor, lists: TensorTable
     if type(lists.c) is not ws_tensor_table or type(drop) is not ws_dropout:
         for x, cls in ((lists.c, ws_tensor_table), (drop, ws_dropout)):
             _refuse(x, cls)
-    _check_flat(plan, r, flat)
+    device = _check_flat(plan, r, flat)
     st = _step().ws_unpack_dropout(plan.handle, r, flat.data_ptr(), _dtype_code(flat.dtype), C.addressof(lists.c),
-                                   C.addressof(drop), _stream())
+                                   C.addressof(drop), _raw_stream(device))
     if st:
         raise WsError(st, "ws_unpack_dropout")
 
@@ -761,9 +767,9 @@ def ws_reduce_dropout(plan: Plan, r: int, grads: TensorTable, drop: ws_dropout, 
     if type(grads.c) is not ws_tensor_table or type(drop) is not ws_dropout:
         for x, cls in ((grads.c, ws_tensor_table), (drop, ws_dropout)):
             _refuse(x, cls)
-    _check_flat(plan, r, flat)
+    device = _check_flat(plan, r, flat)
     st = _step().ws_reduce_dropout(plan.handle, r, C.addressof(grads.c), C.addressof(drop), flat.data_ptr(),
-                                   _dtype_code(flat.dtype), _stream())
+                                   _dtype_code(flat.dtype), _raw_stream(device))
     if st:
         raise WsError(st, "ws_reduce_dropout")
 
@@ -785,23 +791,26 @@ class RouterSet:
         c = self.c = ws_router_set(layers=layers, replicas=replicas, experts=experts, topk=1)
         self._keep = keep = []
 
+        index = self._index = self.device.index if self.device.type == "cuda" else -1
+
         def table(name, lists, width):
             if len(lists) != layers or any(len(x) != replicas for x in lists):
                 raise ValueError(f"{name}: one list per layer with one tensor per replica")
             flat = [t for x in lists for t in x]
-            for i, t in enumerate(flat):
-                if t.dim() != 2 or t.shape[0] != tokens[i % replicas] or t.shape[1] != width:
-                    raise ValueError(f"{name}: [{tokens[i % replicas]}, {width}] expected, not {tuple(t.shape)}")
-                if t.dtype != flat[0].dtype or t.device != self.device:
-                    raise ValueError(f"{name}: tensors of one type on one device")
-            arr = _ptr_array(flat)
+            dtype, shapes = flat[0].dtype, [(n, width) for n in tokens] * layers
+            if any(t.shape != want for t, want in zip(flat, shapes)):
+                raise ValueError(f"{name}: [tokens, {width}] expected, tokens of the replicas {tokens[:8]}")
+            if any(t.dtype is not dtype or t.get_device() != index for t in flat):
+                raise ValueError(f"{name}: tensors of one type on one device")
+            arr = array("Q", [t.data_ptr() for t in flat])
             keep.extend((flat, arr))
-            return flat, C.cast(arr, C.POINTER(C.c_void_p))
+            return flat, C.cast(arr.buffer_info()[0], C.POINTER(C.c_void_p))
 
         def stride(name, flat):
             """Elements from row to row, the same for all tensors of more than one row."""
-            lds = {t.stride(0) for t in flat if t.shape[0] > 1} or {max(1, experts)}
-            if len(lds) > 1 or any(experts > 1 and t.numel() and t.stride(1) != 1 for t in flat):
+            steps = [(t.stride(), n) for t, n in zip(flat, tokens * layers)]
+            lds = {st[0] for st, n in steps if n > 1} or {max(1, experts)}
+            if len(lds) > 1 or experts > 1 and any(n and st[1] != 1 for st, n in steps):
                 raise ValueError(f"{name}: contiguous rows at one stride expected")
             return lds.pop()
 
@@ -833,7 +842,6 @@ class RouterSet:
                 arr[k] = t.data_ptr()
             keep.extend((list(valid), arr))
             c.valid = C.cast(arr, C.POINTER(C.c_void_p))
-        self._index = self.device.index if self.device.type == "cuda" else -1
         self._counts_shape, self._loss_shape = (layers, self.experts + 1), (layers, 2)
         self._tokens = (C.c_int64 * replicas)(*tokens)
         c.tokens = C.cast(self._tokens, C.POINTER(C.c_int64))
@@ -857,7 +865,8 @@ def _router_addr(routers, counts):
 def ws_router_counts(routers: RouterSet, counts: torch.Tensor, accumulate: bool = False):
     """counts[l] = picks of every expert of layer l over all replicas' valid tokens, and as its last entry their number
     (``accumulate``: added to what counts holds)."""
-    st = _step().ws_router_counts(_router_addr(routers, counts), counts.data_ptr(), 1 if accumulate else 0, _stream())
+    st = _step().ws_router_counts(_router_addr(routers, counts), counts.data_ptr(), 1 if accumulate else 0,
+                                  _raw_stream(routers._index))
     if st:
         raise WsError(st, "ws_router_counts")
 
@@ -878,6 +887,6 @@ def ws_balance_loss(routers: RouterSet, counts: torch.Tensor, loss: Optional[tor
     st = _step().ws_balance_loss(addr, counts.data_ptr(), loss.data_ptr() if loss is not None else None, coef, z_coef,
                                  upstream.data_ptr() if upstream is not None else None, 1 if accumulate else 0,
                                  workspace.data_ptr() if workspace is not None else None,
-                                 workspace.nbytes if workspace is not None else 0, _stream())
+                                 workspace.nbytes if workspace is not None else 0, _raw_stream(routers._index))
     if st:
         raise WsError(st, "ws_balance_loss")
