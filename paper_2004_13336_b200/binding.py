@@ -778,12 +778,16 @@ class RouterSet:
     """The routers' tensors of a training step for ws_router_counts and ws_balance_loss: nested lists, one inner list per
     layer with one tensor per replica.  ``picks``: integers [tokens, topk]; ``logits`` and ``dlogits``: [tokens, experts]
     with contiguous rows (a common row stride); ``valid``: None, or one bool or byte tensor [tokens] (or None) per
-    replica.  Keeps the tensors and the C arrays, so that a call of every step costs one ctypes call."""
+    replica.  Without picks (for ws_balance_loss alone) ``topk`` says how many a token has.  Keeps the tensors and the C
+    arrays, so that a call of every step costs one ctypes call."""
 
-    def __init__(self, experts: int, picks=None, valid=None, logits=None, dlogits=None, score: str = "softmax"):
+    def __init__(self, experts: int, picks=None, valid=None, logits=None, dlogits=None, score: str = "softmax",
+                 topk: Optional[int] = None):
         like = picks if picks is not None else logits
         if not like or not like[0]:
             raise ValueError("a router set has picks or logits of one layer and one replica at least")
+        if any(t.dim() != 2 for t in like[0]):
+            raise ValueError("picks and logits have a row for every token")
         layers, replicas = len(like), len(like[0])
         tokens = [t.shape[0] for t in like[0]]
         self.experts, self.layers, self.replicas = int(experts), layers, replicas
@@ -814,7 +818,13 @@ class RouterSet:
                 raise ValueError(f"{name}: contiguous rows at one stride expected")
             return lds.pop()
 
+        if topk is not None:
+            c.topk = topk
+        elif picks is None:
+            raise ValueError("a router set without picks needs topk")
         if picks is not None:
+            if topk is not None and topk != picks[0][0].shape[1]:
+                raise ValueError(f"topk is {topk}, a row of picks {picks[0][0].shape[1]}")
             c.topk = picks[0][0].shape[1]
             flat, c.picks = table("picks", picks, c.topk)
             if flat[0].dtype not in (torch.int32, torch.int64) or not all(t.is_contiguous() for t in flat):

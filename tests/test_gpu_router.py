@@ -328,8 +328,7 @@ def test_offsets_past_32_bits():
     ws = torch.empty(routers.workspace_bytes(), dtype=torch.uint8, device=DEV)
     B.ws_balance_loss(routers, counts, loss, 1e-2, workspace=ws)
     tail = torch.empty(300, experts, dtype=BF16, device=DEV)
-    part = B.RouterSet(experts, None, None, [[x[-300:]]], [[tail]])
-    part.c.topk = 2
+    part = B.RouterSet(experts, None, None, [[x[-300:]]], [[tail]], topk=2)
     B.ws_balance_loss(part, counts, None, 1e-2, workspace=ws)
     assert torch.equal(tail, d[-300:])
     f = want.double() / (2 * n)

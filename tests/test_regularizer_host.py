@@ -224,18 +224,20 @@ def test_router_set_refuses_tensors_that_do_not_belong_together():
     i = lambda n, k=2: torch.zeros(n, k, dtype=torch.int64)  # noqa: E731
     x = lambda n, e=8: torch.zeros(n, e)  # noqa: E731
     B.RouterSet(8, [[i(3), i(0)], [i(3), i(0)]], [torch.ones(3, dtype=torch.bool), None], [[x(3), x(0)], [x(3), x(0)]])
-    B.RouterSet(8, logits=[[torch.zeros(3, 16)[:, :8]]], dlogits=[[x(3)]])
-    for bad in (lambda: B.RouterSet(8), lambda: B.RouterSet(8, []), lambda: B.RouterSet(8, [[]]),
+    B.RouterSet(8, logits=[[torch.zeros(3, 16)[:, :8]]], dlogits=[[x(3)]], topk=2)
+    assert B.RouterSet(8, [[i(3)]], topk=2).c.topk == B.RouterSet(8, logits=[[x(3)]], topk=2).c.topk == 2
+    for bad in (lambda: B.RouterSet(8), lambda: B.RouterSet(8, [[torch.zeros(3, dtype=torch.int64)]]), lambda: B.RouterSet(8, []), lambda: B.RouterSet(8, [[]]),
                 lambda: B.RouterSet(8, [[i(3), i(4)], [i(3)]]), lambda: B.RouterSet(8, [[i(3), i(4)], [i(3), i(5)]]),
-                lambda: B.RouterSet(8, [[i(3)]], logits=[[x(4)]]), lambda: B.RouterSet(8, logits=[[x(3, 7)]]),
+                lambda: B.RouterSet(8, [[i(3)]], logits=[[x(4)]]), lambda: B.RouterSet(8, logits=[[x(3, 7)]], topk=2),
+                lambda: B.RouterSet(8, logits=[[x(3)]]), lambda: B.RouterSet(8, [[i(3)]], topk=3),
                 lambda: B.RouterSet(8, [[i(3)]], dlogits=[[x(3)]]), lambda: B.RouterSet(8, [[i(3)]], valid=[torch.ones(4, dtype=torch.bool)]),
                 lambda: B.RouterSet(8, [[i(3)]], valid=[torch.ones(3)]), lambda: B.RouterSet(8, [[i(3)]], valid=[]),
-                lambda: B.RouterSet(8, logits=[[torch.zeros(8, 3).t()]]), lambda: B.RouterSet(8, logits=[[x(3), torch.zeros(3, 16)[:, :8]]]),
-                lambda: B.RouterSet(8, logits=[[x(3), x(3).bfloat16()]])):
+                lambda: B.RouterSet(8, logits=[[torch.zeros(8, 3).t()]], topk=2), lambda: B.RouterSet(8, logits=[[x(3), torch.zeros(3, 16)[:, :8]]], topk=2),
+                lambda: B.RouterSet(8, logits=[[x(3), x(3).bfloat16()]], topk=2)):
         with pytest.raises(ValueError):
             bad()
     for bad in (lambda: B.RouterSet(8, [[i(3).to(torch.int16)]]), lambda: B.RouterSet(8, [[torch.zeros(3, 4, dtype=torch.int64)[:, :2]]]),
-                lambda: B.RouterSet(8, logits=[[x(3).half()]]), lambda: B.RouterSet(8, logits=[[x(3)]], dlogits=[[x(3).bfloat16()]])):
+                lambda: B.RouterSet(8, logits=[[x(3).half()]], topk=2), lambda: B.RouterSet(8, logits=[[x(3)]], dlogits=[[x(3).bfloat16()]], topk=2)):
         with pytest.raises(TypeError):
             bad()
     routers = B.RouterSet(8, [[i(3)]])
