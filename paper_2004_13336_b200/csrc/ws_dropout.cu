@@ -327,10 +327,11 @@ void launch(void (*kernel)(KArgs...), long long grid, int block, cudaStream_t st
     cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
 }
 
-// How a call's tiles are cut up: tiles, elements of the plan's tile, a warp per tile or a CTA.
+// How a call's tiles are cut up: tiles, elements of the plan's tile and of the average one, a warp per tile or a CTA.
 struct Shape {
     long long items;
     int tile;
+    long long average;
     bool is_short;
 };
 // CTAs of `most` threads, fewer where a tile would not give each of them `unroll` vectors.
@@ -355,7 +356,10 @@ template <bool FBF, bool TBF, bool WIDE, bool SHORT>
 void launch_op(bool sum, void* flat, const Shape& s, cudaStream_t st, const DropParams& P) {
     const void* from = flat;
     if (!sum) {
-        if (FBF && TBF) launch_tiles(hand_out_kernel<FBF, TBF, WIDE, SHORT, 4, 5>, s, 64, 4, st, P, from);
+        // Four vectors in flight need tiles that have them; without, with many lists, a draw's latency is all there is (us, 4 / 1:
+        // 16 lists of 2 M in 64 shards 50 / 29, in 16 shards 42 / 23, 3 lists of 45 M in 64 shards 66 / 72).
+        if (FBF && TBF && (P.nsets <= 3 || s.average >= 1536)) launch_tiles(hand_out_kernel<FBF, TBF, WIDE, SHORT, 4, 5>, s, 64, 4, st, P, from);
+        else if (FBF && TBF) launch_tiles(hand_out_kernel<FBF, TBF, WIDE, SHORT, 1, 5>, s, 64, 1, st, P, from);
         else if (P.nsets == 1) launch_tiles(hand_out_kernel<FBF, TBF, WIDE, SHORT, 2, 3>, s, 64, 2, st, P, from);
         else launch_tiles(hand_out_kernel<FBF, TBF, WIDE, SHORT, 2, 1>, s, 128, 2, st, P, from);
     } else if (P.nsets == 1) {
@@ -421,9 +425,9 @@ ws_status run(bool sum, const ws_plan* p, int32_t r, void* flat, ws_dtype flat_d
     const bool wide = table->min_align >= 32 && (reinterpret_cast<uintptr_t>(flat) & 31u) == 0;
     // A warp per tile where tiles are short and many, and not long enough in any place to leave a warp walking alone (ws_pack's
     // rule, in elements).  us, a CTA / a warp per tile: 64 shards of 47 M in tiles of 900, sum of one bf16 list 56 / 40, fp32 to one
-    // list 61 / 60; 16 bf16 lists of 4 M in tiles of 660, whose draws are enough work for a CTA, 38 / 50.
+    // list 61 / 60; 16 bf16 lists of 4 M in tiles of 660, whose draws are enough work for a CTA, 38 / 50, 8 of 2 M 15 / 22.
     const long long tile = p->ntiles > 0 ? (P.concat ? p->S * p->R : p->S) / p->ntiles : p->K;
-    const Shape s{P.nitems, p->K, P.nitems > 32LL * p->sms && tile <= (P.nsets <= 2 ? 1024 : P.nsets <= 8 ? 768 : 0) && p->longest <= 128 << 10};
+    const Shape s{P.nitems, p->K, tile, P.nitems > 32LL * p->sms && tile <= (P.nsets <= 2 ? 1024 : P.nsets <= 4 ? 768 : 256) && p->longest <= 128 << 10};
     cudaStream_t st = (cudaStream_t)stream;
     if (flat_dtype == WS_BF16) (table->dtype == WS_BF16 ? launch_types<true, true> : launch_types<true, false>)(sum, wide, flat, s, st, P);
     else (table->dtype == WS_BF16 ? launch_types<false, true> : launch_types<false, false>)(sum, wide, flat, s, st, P);
