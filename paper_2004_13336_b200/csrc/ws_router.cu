@@ -436,7 +436,7 @@ __global__ void __launch_bounds__(kBlock, balance_ctas(C * V, SIG)) balance_kern
                 };
                 F2 s[H], y[SIG ? H : 1];
                 float total, inner, shift = 0.f;
-                // exp(v - shift), also where v log2 e would leave fp32's range
+                // exp(v - shift) with the difference formed first: right for any v and shift
                 auto far_exponentials = [&] {
 #pragma unroll
                     for (int h = 0; h < H; ++h) s[h] = F2(exp2_fast((get(2 * h) - shift) * kLog2e), exp2_fast((get(2 * h + 1) - shift) * kLog2e));
@@ -491,7 +491,11 @@ __global__ void __launch_bounds__(kBlock, balance_ctas(C * V, SIG)) balance_kern
                     }
                 } else {
                     shift = row_top();
-                    if (__any_sync(0xffffffffu, !(fabsf(shift) < 1e37f))) {
+                    // v log2 e - shift log2 e in one fma, whose second term is rounded: every exponent of the row is off by half
+                    // a unit in the last place of it, the same for all, so the scores' ratios stay and the sum's logarithm
+                    // moves by less than shift's own rounding.  Below 2^20 that is 2^-4 at most; from some 2^31 on the
+                    // scores would all vanish or overflow.
+                    if (__any_sync(0xffffffffu, !(fabsf(shift) < 1048576.f))) {
                         far_exponentials();
                     } else {
                         const float bias = -shift * kLog2e;

@@ -1,0 +1,57 @@
+"""The balance loss and its gradient at logits and factors far from 1, against plain forms in 64 bits.
+
+Tolerances as derived in tests/test_gpu_router.py (K of the parts' magnitudes, the types' roundings).  A score that counts as 0
+is below 2^-126 of its row's largest; its gradient is that times the row's factors, which are not below 1 here: `factor`."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2004_13336_b200 import binding as B
+from tests import _regularizer_ref as R
+from tests.test_gpu_router import BF16, DEV, F32, K, TINY, f64, make, np_lists, np_valid
+from tests._util import to_np
+
+pytestmark = pytest.mark.gpu
+
+
+def call(picks, logits, dlogits, valid, experts, score="softmax", coef=1e-2, z=0.0, upstream=None, loss=True):
+    routers = B.RouterSet(experts, picks, valid, logits, dlogits, score)
+    counts = torch.empty(len(logits), experts + 1, dtype=torch.int64, device=DEV)
+    B.ws_router_counts(routers, counts)
+    got = torch.full((len(logits), 2), float("nan"), device=DEV) if loss else None
+    ws = torch.full((routers.workspace_bytes(),), 255, dtype=torch.uint8, device=DEV)
+    B.ws_balance_loss(routers, counts, got, coef, z, upstream, False, ws)
+    return got, counts
+
+
+def expect_gradient(t, want, size, factor):
+    bound = K * size
+    bound = bound + torch.finfo(t.dtype).eps / 2 * (np.abs(want) + bound) + TINY * factor
+    assert (np.abs(f64(t) - want) <= bound).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("top", [1e3, -1e4, 1.04e6, -1.06e6, 3e8, -3e8, 6e9, -6e9, 1e10, -1e10, 1e15, -1e15, -1e30, 9e36, -9e36, 2e38])
+def test_rows_whose_largest_logit_is_far_from_zero(top, dtype):
+    """Experts masked with a large finite number, rows of nothing else among them: they are a softmax like any other.  The z loss
+    where the logits' squares and their sum are fp32 numbers."""
+    picks, logits, dlogits, _, _ = make(1, [40], 32, 2, dtype)
+    x = logits[0][0]
+    x[0] = top
+    x[1, ::2] = top
+    x[2, 3:] = top
+    x[3] = top
+    x[3, 7] = -float("inf")
+    x[4] = -abs(top)
+    x[4, 9] = abs(top)
+    # distinct logits next to the largest one, some units of the type's last place apart
+    x[5:8] = (top + abs(top) * torch.finfo(dtype).eps * torch.arange(-48, 48, device=DEV).view(3, 32)).to(dtype)
+    z = 1e-3 if abs(top) <= 1e15 else 0.0
+    got, counts = call(picks, logits, dlogits, None, 32, z=z)
+    ref, grads, sizes = R.balance(np_lists(logits), None, to_np(counts), 2, "softmax", 1e-2, z)
+    # the row's factors 2 z / N |lse| + coef E / N (N = 40), and 2^(2^-4) where all exponents of a row are off by 2^-4
+    expect_gradient(dlogits[0][0], grads[0][0], sizes[0][0], 2 ** 0.0625 * (2 * z / 40 * (abs(top) * 1.01 + 4) + 0.008))
+    _, lse, _, far = R.scores(f64(x), "softmax")
+    bound = K * np.array([ref[0, 0], 2 * z / 40 * (np.abs(lse) * (np.abs(lse) + far + 1)).sum()]) + 2.0 ** -24 * ref[0]
+    assert (np.abs(f64(got)[0] - ref[0]) <= bound).all()
+    assert bool(torch.isfinite(got).all()) and bool(torch.isfinite(dlogits[0][0]).all())
