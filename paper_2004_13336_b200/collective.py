@@ -56,7 +56,10 @@ class ShardedUpdate:
         if opt in ("lamb", "lars", "adafactor"):
             self.workspace = torch.zeros(max(16, self.plan.workspace_bytes(opt)), dtype=torch.uint8,
                                          device=self.device)
-        self.dropout, self.drawn = dropout, 0             # masks handed out last: those of step `drawn`
+        self.dropout = dropout
+        # Masks handed out last: those of step `drawn`.  A word beside the weights, counted up on the stream of the steps,
+        # so that a captured step draws new masks at each replay.
+        self._drawn = torch.zeros(1, dtype=torch.int32, device=self.device)
         self.fstate = None                                                    # Adafactor: replicated, small
         if opt == "adafactor":
             self.fstate = torch.zeros(self.plan.factored_elems, **z)
@@ -79,9 +82,20 @@ class ShardedUpdate:
     def _table(self, tensors):
         return tensors if isinstance(tensors, self.ops.TensorTable) else self.ops.TensorTable(self.plan, [list(tensors)])
 
-    def _masks(self, step: int):
+    @property
+    def drawn(self) -> int:
+        """The step whose masks were handed out last (modulo 2^32).  Reading it waits for the steps in flight."""
+        return int(self._drawn) & 0xFFFFFFFF
+
+    @drawn.setter
+    def drawn(self, step: int):
+        self._drawn.fill_((int(step) + (1 << 31)) % (1 << 32) - (1 << 31))
+
+    def _masks(self):
         p, seed = self.dropout
-        return self.ops.make_dropout(p, seed, step, self.rank)
+        if self._drawn.is_cuda:
+            return self.ops.make_dropout(p, seed, 0, self.rank, self._drawn)
+        return self.ops.make_dropout(p, seed, self.drawn, self.rank)
 
     def hand_out(self, weights_out):
         """Gathers the present weights and hands this replica's part of them out, under the masks that the next
@@ -89,13 +103,14 @@ class ShardedUpdate:
         S, r = self.plan.S, self.rank
         self.gathered[r * S:(r + 1) * S].copy_(self.w)
         dist.all_gather_into_tensor(self.gathered, self.gathered[r * S:(r + 1) * S], group=self.group)
-        self.ops.ws_unpack_dropout(self.plan, -1, self.gathered, self._table(weights_out), self._masks(self.drawn))
+        self.ops.ws_unpack_dropout(self.plan, -1, self.gathered, self._table(weights_out), self._masks())
 
     def step(self, grads: Sequence[torch.Tensor], weights_out: Sequence[torch.Tensor], step: Optional[int] = None):
         """One training step's weight update.  ``grads``: this replica's local gradients, one tensor
         per model tensor.  ``weights_out``: the model's weight tensors (``out_dtype``), overwritten
         with the updated full weights (with ``dropout``: this replica's next part of them; both may then be
-        tables made once, ``ops.TensorTable(su.plan, [tensors])``, and are where the step is captured)."""
+        tables made once, ``ops.TensorTable(su.plan, [tensors])``, and are where the step is captured in a CUDA graph: every
+        replay takes the masks one step on, and repeats the optimizer's constants, its step number among them)."""
         ops, plan, r, S = self.ops, self.plan, self.rank, self.plan.S
         if step is not None:
             self.hyper_dict["step"] = step
@@ -103,7 +118,7 @@ class ShardedUpdate:
         if self.dropout is None:
             ops.ws_pack(plan, grads, self.packed)                               # formatting (Section 5.1)
         else:                                                                   # ... under this replica's masks
-            ops.ws_reduce_dropout(plan, -1, self._table(grads), self._masks(self.drawn), self.packed)
+            ops.ws_reduce_dropout(plan, -1, self._table(grads), self._masks(), self.packed)
         dist.reduce_scatter_tensor(self.recv, self.packed, op=dist.ReduceOp.SUM, group=self.group)
         if self.opt == "lamb":
             ops.ws_lamb_partial(plan, r, [self.recv], self.w, self.m, self.v, hy, self.workspace, slice_mode=1)
@@ -138,8 +153,8 @@ class ShardedUpdate:
         if self.dropout is None:
             ops.ws_unpack(plan, self.gathered, weights_out)                     # reverse formatting
         else:
-            self.drawn += 1
-            ops.ws_unpack_dropout(plan, -1, self.gathered, self._table(weights_out), self._masks(self.drawn))
+            self._drawn.add_(1)
+            ops.ws_unpack_dropout(plan, -1, self.gathered, self._table(weights_out), self._masks())
 
 
 class ExpertBalance:

@@ -1,0 +1,67 @@
+"""The framework's own paths captured in CUDA graphs and replayed, on a one-rank NCCL group."""
+import socket
+
+import numpy as np
+import pytest
+import torch
+import torch.distributed as dist
+
+from tests import _regularizer_ref as R
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+SHAPES = [(1,), (7,), (3, 3, 16, 32), (64, 128), (1031,), (0, 3), (300, 301)]
+
+
+@pytest.fixture(scope="module")
+def world_of_one():
+    with socket.socket() as s:
+        s.bind(("127.0.0.1", 0))
+        port = s.getsockname()[1]
+    torch.cuda.set_device(0)
+    dist.init_process_group("nccl", init_method=f"tcp://127.0.0.1:{port}", rank=0, world_size=1)
+    yield
+    dist.destroy_process_group()
+
+
+def test_replayed_step_with_dropout_draws_new_masks(world_of_one):
+    """Eager steps and replays in turn follow the plain run, whose masks move on by one with every step."""
+    from paper_2004_13336_b200 import binding as B
+    from paper_2004_13336_b200.collective import ShardedUpdate
+    p, seed = 0.2, 31
+    n = [int(np.prod(s)) for s in SHAPES]
+    gen = torch.Generator(device=DEV).manual_seed(2)
+    w0 = [torch.empty(k, device=DEV).normal_(generator=gen) for k in n]
+    zero = [torch.zeros(k, device=DEV) for k in n]
+    hyper = dict(lr=0.1, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, momentum=0.9, grad_scale=1.0, step=1)
+    su = ShardedUpdate(SHAPES, "sgdm", hyper, device=DEV, dropout=(p, seed))
+    su.load_state(w0, zero, zero)
+    weights, grads = ([torch.zeros(k, device=DEV) for k in n] for _ in range(2))
+    wt, gt = B.TensorTable(su.plan, [weights]), B.TensorTable(su.plan, [grads])
+    w, m = [t.double().cpu().numpy() for t in w0], [np.zeros(k) for k in n]
+    su.hand_out(wt)
+    graph = torch.cuda.CUDAGraph()
+    try:
+        for step in range(7):
+            for t in range(len(n)):
+                want = R.hand_out(w[t], p, seed, step, 0, t)
+                got = weights[t].double().cpu().numpy()
+                # a few fp32 roundings a step (2^-22 of values below 8), the scale and its product two more
+                assert (np.abs(got - want) <= 2.0 ** -17).all() and ((got == 0) == (want == 0)).all(), (step, t)
+            assert su.drawn == step
+            for t in range(len(n)):
+                grads[t].normal_(generator=gen)
+                g, _ = R.masked_sum([grads[t].cpu().numpy()], p, seed, step, 0, t)
+                m[t] = 0.9 * m[t] + g
+                w[t] = w[t] - 0.1 * m[t]
+            if step == 1:
+                torch.cuda.synchronize()
+                with torch.cuda.graph(graph, capture_error_mode="thread_local"):
+                    su.step(gt, wt)
+            if step in (0, 4):
+                su.step(gt, wt)
+            else:
+                graph.replay()
+        torch.cuda.synchronize()
+    finally:
+        graph.reset()           # it holds the group's collectives
