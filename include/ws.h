@@ -458,7 +458,9 @@ ws_status ws_workspace_adafactor_sums(const ws_plan* plan, size_t* offset_bytes,
  *   fills *out, which the caller passes to ws_fused_update and keeps alive,
  *   together with the device buffer, while it is in use.  Every tensor pointer
  *   must be 16-byte aligned; 32-byte alignment of all of them lets the kernels
- *   use 256-bit accesses.
+ *   use 256-bit accesses.  On a stream that is being captured the call is
+ *   refused with WS_ERR_INVALID_ARG (a captured copy would read the host side
+ *   of it again at every replay): upload before the capture.
  * The tensors may live in any memory the device can address, pinned host
  * memory included: the kernel then pulls the gradients over PCIe itself and
  * writes the weights back the same way, with no staging copy (the table

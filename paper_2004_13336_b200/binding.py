@@ -652,7 +652,8 @@ def ws_lamb_update_static_scratch(plan: Plan, gbufs, w, m, v, hyper: ws_hyper,
 
 class TensorTable:
     """Device-resident table of tensor pointers for ws_fused_update: `sets` is a list of
-    tensor lists (R gradient lists, or one weight list).  Keeps the device buffer alive."""
+    tensor lists (R gradient lists, or one weight list).  Keeps the device buffer alive.  Made before a
+    capture, never in one (refused)."""
 
     def __init__(self, plan: Plan, sets: Sequence[Sequence[torch.Tensor]], device=None):
         nsets = len(sets)

@@ -1045,6 +1045,11 @@ extern "C" ws_status ws_tensor_table_upload(const ws_plan* plan, const void* con
     if (dtype != WS_F32 && dtype != WS_BF16) return WS_ERR_DTYPE;
     if (!ws_aligned16(dev_buf)) return WS_ERR_ALIGNMENT;
     if (bytes < ws_tensor_table_bytes(plan, nsets)) return WS_ERR_WORKSPACE;
+    // A captured copy reads its source at every replay, and `host` is gone when this call returns.
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    const cudaError_t asked = cudaStreamIsCapturing((cudaStream_t)stream, &capture);
+    if (asked != cudaSuccess) return ws_cuda_fail(asked, "ws_tensor_table_upload");
+    if (capture != cudaStreamCaptureStatusNone) return WS_ERR_INVALID_ARG;
     const int T = plan->T;
     std::vector<const void*> host((size_t)T * nsets);
     int min_align = 256;

@@ -65,3 +65,34 @@ def test_replayed_step_with_dropout_draws_new_masks(world_of_one):
         torch.cuda.synchronize()
     finally:
         graph.reset()           # it holds the group's collectives
+
+
+def test_tables_are_not_made_in_a_capture(world_of_one):
+    """The upload of a table in a capture would read freed host memory at replay: refused, by itself and where a step is given
+    plain lists; the capture goes on, and a step with tables made before it replays."""
+    from paper_2004_13336_b200 import binding as B
+    from paper_2004_13336_b200.collective import ShardedUpdate
+    n = [int(np.prod(s)) for s in SHAPES]
+    hyper = dict(lr=0.5, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, momentum=0.0, grad_scale=1.0, step=1)
+    su = ShardedUpdate(SHAPES, "sgdm", hyper, device=DEV, dropout=(0.0, 3))
+    w0, zero = [torch.randn(k, device=DEV) for k in n], [torch.zeros(k, device=DEV) for k in n]
+    su.load_state(w0, zero, zero)
+    weights, grads = [torch.zeros(k, device=DEV) for k in n], [torch.randn(k, device=DEV) for k in n]
+    wt, gt = B.TensorTable(su.plan, [weights]), B.TensorTable(su.plan, [grads])
+    su.step(gt, wt)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    try:
+        with torch.cuda.graph(graph, capture_error_mode="thread_local"):
+            for call in (lambda: B.TensorTable(su.plan, [weights]), lambda: su.step(grads, wt),
+                         lambda: B.TensorTable.from_pointers(su.plan, [[t.data_ptr() for t in weights]], torch.float32, DEV)):
+                with pytest.raises(B.WsError) as e:
+                    call()
+                assert e.value.status == 1
+            su.step(gt, wt)
+        for k in range(2, 5):
+            graph.replay()
+            for a, b, g in zip(weights, w0, grads):      # values below 16: three roundings of 2^-21 a step
+                assert bool(((a.double() - b.double() + 0.5 * k * g.double()).abs() <= k * 3 * 2.0 ** -21).all())
+    finally:
+        graph.reset()
