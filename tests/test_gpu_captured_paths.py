@@ -96,3 +96,34 @@ def test_tables_are_not_made_in_a_capture(world_of_one):
                 assert bool(((a.double() - b.double() + 0.5 * k * g.double()).abs() <= k * 3 * 2.0 ** -21).all())
     finally:
         graph.reset()
+
+
+def _routers(B, tokens, experts, seed):
+    gen = torch.Generator(device=DEV).manual_seed(seed)
+    logits = [[torch.empty(tokens, experts, device=DEV).normal_(generator=gen)] for _ in range(2)]
+    picks = [[torch.topk(t[0], 2, dim=1).indices] for t in logits]
+    return B.RouterSet(experts, picks, None, logits, [[torch.empty_like(t[0])] for t in logits])
+
+
+def test_replayed_balance_keeps_to_its_own_memory(world_of_one):
+    """A captured step, then one that needs more scratch, then replays: they give the loss, and write to nobody else's memory."""
+    from paper_2004_13336_b200 import binding as B
+    from paper_2004_13336_b200.collective import ExpertBalance
+    balance = ExpertBalance(2, 64, 0.01, 1e-3)
+    small, large = _routers(B, 3000, 64, 1), _routers(B, 60000, 64, 2)
+    assert small.workspace_bytes() < large.workspace_bytes()
+    want = balance.step(small).clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    try:
+        with torch.cuda.graph(graph, capture_error_mode="thread_local"):
+            loss = balance.step(small)
+        balance.step(large)
+        others = [torch.full((small.workspace_bytes(),), 0x5A, dtype=torch.uint8, device=DEV) for _ in range(3000)]
+        for _ in range(3):
+            loss.fill_(9)
+            graph.replay()
+            assert torch.equal(loss, want)
+        assert all(bool((t == 0x5A).all()) for t in others)
+    finally:
+        graph.reset()
