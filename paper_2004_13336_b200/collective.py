@@ -168,15 +168,17 @@ class ExpertBalance:
         self.ops, self.coef, self.z_coef, self.group = ops, coef, z_coef, group
         device = torch.device(device) if device is not None else torch.device("cuda", torch.cuda.current_device())
         self.counts = torch.zeros(layers, experts + 1, dtype=torch.int64, device=device)
-        self.loss = torch.zeros(layers, 2, device=device)
+        self.loss = torch.zeros(layers, 2, device=device)            # what the last step returned
 
     def step(self, routers, upstream: Optional[torch.Tensor] = None, accumulate: bool = False) -> torch.Tensor:
         """``routers``: this replica's tensors (``ops.RouterSet``, with one replica's lists).  Fills their dlogits and
-        returns the batch's losses [layers][2]; ``self.counts`` holds the batch's counts, the tokens' number last."""
+        returns the batch's losses [layers][2], a new tensor for each call; ``self.counts`` holds the batch's counts until
+        the next one, the tokens' number last."""
         # scratch of this call: one kept here and replaced by a larger one would be gone under a captured step
         workspace = torch.empty(max(16, routers.workspace_bytes()), dtype=torch.uint8, device=self.counts.device)
         self.ops.ws_router_counts(routers, self.counts)
         dist.all_reduce(self.counts, group=self.group)
+        self.loss = torch.empty_like(self.loss)
         self.ops.ws_balance_loss(routers, self.counts, self.loss, self.coef, self.z_coef, upstream, accumulate, workspace)
         dist.all_reduce(self.loss, group=self.group)
         return self.loss
