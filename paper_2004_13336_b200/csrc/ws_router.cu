@@ -519,8 +519,9 @@ __global__ void __launch_bounds__(kBlock, balance_ctas(C * V, SIG)) balance_kern
                 }
                 if (out) {
                     if (i0 + sub < n && (live || !P.accumulate)) {
-                        // p_e (slope (f_e - inner) + zslope lse) with p_e = s_e scale; a token that does not exist has scores 0
-                        const float a = slope * scale, b = (SIG ? -slope * inner : zslope * lse - slope * inner) * scale;
+                        // p_e (slope (f_e - inner) + zslope lse) with p_e = s_e scale; a token that does not exist has scores 0, and
+                        // no factors either: an infinite one (an overflowed loss scale) would make NaN of them
+                        const float a = empty ? 0.f : slope * scale, b = empty ? 0.f : (SIG ? -slope * inner : zslope * lse - slope * inner) * scale;
                         float d[2 * H];
 #pragma unroll
                         for (int h = 0; h < H; ++h) {

@@ -55,3 +55,26 @@ def test_rows_whose_largest_logit_is_far_from_zero(top, dtype):
     bound = K * np.array([ref[0, 0], 2 * z / 40 * (np.abs(lse) * (np.abs(lse) + far + 1)).sum()]) + 2.0 ** -24 * ref[0]
     assert (np.abs(f64(got)[0] - ref[0]) <= bound).all()
     assert bool(torch.isfinite(got).all()) and bool(torch.isfinite(dlogits[0][0]).all())
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("up", [float("inf"), -float("inf"), float("nan")])
+def test_factors_that_are_no_numbers_leave_rows_without_scores_at_0(up, dtype, score):
+    """An overflowed loss scale shows in the valid rows; masked tokens and rows that leave no expert have gradient 0, and a layer
+    without tokens has nothing else."""
+    for experts, tokens in ((24, [90, 33]), (33, [90, 33]), (64, [3000, 10])):
+        picks, logits, dlogits, valid, _ = make(2, tokens, experts, 2, dtype, valid=0.8)
+        empty = torch.zeros(tokens[0], dtype=torch.bool, device=DEV)
+        empty[::7] = True
+        for layer in logits:
+            layer[0][empty] = -float("inf")
+        z = 1e-3 if score == "softmax" else 0.0
+        call(picks, logits, dlogits, valid, experts, score, z=z, upstream=torch.tensor([up], device=DEV))
+        for layer in dlogits:
+            gone = empty | ~valid[0]
+            assert bool((layer[0][gone] == 0).all()) and not bool(torch.isfinite(layer[0][~gone]).all(1).any())
+            assert not bool(torch.isfinite(layer[1]).all(1).any())
+        none = [torch.zeros(n, dtype=torch.uint8, device=DEV) for n in tokens]
+        call(picks, logits, dlogits, none, experts, score, z=z, upstream=torch.tensor([up], device=DEV))
+        assert not any(bool(t.any()) for layer in dlogits for t in layer)
