@@ -667,8 +667,8 @@ ws_status ws_reduce_dropout(const ws_plan* plan, int32_t r, const ws_tensor_tabl
  * nothing to either loss and has gradient 0.  NaN or (WS_SOFTMAX) +infinity in a valid row gives NaN.  A layer
  * without tokens has loss and gradient 0.
  *   coef, z_coef  finite; z_coef must be 0 with WS_SIGMOID
- *   upstream      device float u, or NULL for 1.  Where u coef experts / N or u z_coef / N is no finite fp32
- *                 number the rows of valid tokens with an expert to pick hold infinities and
+ *   upstream      device float u, or NULL for 1.  u coef experts / N and u z_coef / N are formed in 64 bits; where
+ *                 they are no finite fp32 numbers the rows of valid tokens with an expert to pick hold infinities and
  *                 NaN, all others 0 as ever
  *   workspace     device scratch of ws_balance_workspace_bytes(set) bytes, 16-byte aligned; nothing in it
  *                 has to be cleared.  Calls that can run at the same time need one each.

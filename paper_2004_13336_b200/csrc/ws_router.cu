@@ -176,7 +176,7 @@ struct BalanceParams {
     double2* partials;             // [layers][slots]
     long long ld, dld;
     double coef, z;
-    float slope, zslope;           // coef experts, 2 z
+    double slope, zslope;          // coef experts, 2 z
     int accumulate;
     int lanes;                     // lanes of a row, a power of two
     int layers;                    // layers of the launch
@@ -401,7 +401,8 @@ __global__ void __launch_bounds__(kBlock, balance_ctas(C * V, SIG)) balance_kern
 
         const long long* counts = P.counts + (long long)(P.r.layer0 + layer) * (E + 1);
         const float tokens = (float)counts[E], inv = tokens > 0.f ? 1.f / tokens : 0.f, inv_picks = inv / P.r.topk;
-        const float slope = up * P.slope * inv, zslope = P.z == 0.0 ? 0.f : up * P.zslope * inv;
+        // (in 64 bits: neither factor needs to be an fp32 number for the product to be one)
+        const float slope = (float)(up * P.slope * inv), zslope = P.z == 0.0 ? 0.f : (float)(up * P.zslope * inv);
         __syncthreads();               // (the layer before is done with its shares)
         for (int e = threadIdx.x; e < C * G * V; e += kBlock) shares[e] = e < E ? (float)counts[e] * inv_picks : 0.f;
         __syncthreads();
@@ -852,8 +853,8 @@ extern "C" ws_status ws_balance_loss(const ws_router_set* s, const int64_t* coun
     P.dld = s->dlogits_ld;
     P.coef = coef;
     P.z = z_coef;
-    P.slope = (float)(coef * s->experts);
-    P.zslope = (float)(2.0 * z_coef);
+    P.slope = coef * s->experts;
+    P.zslope = 2.0 * z_coef;
     P.accumulate = accumulate;
     cudaStream_t st = (cudaStream_t)stream;
     const int most = kMaxPointers / s->replicas;

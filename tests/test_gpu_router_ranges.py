@@ -78,3 +78,16 @@ def test_factors_that_are_no_numbers_leave_rows_without_scores_at_0(up, dtype, s
         none = [torch.zeros(n, dtype=torch.uint8, device=DEV) for n in tokens]
         call(picks, logits, dlogits, none, experts, score, z=z, upstream=torch.tensor([up], device=DEV))
         assert not any(bool(t.any()) for layer in dlogits for t in layer)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_coefficients_past_fp32_with_a_small_factor(score):
+    """coef and z_coef are 64-bit numbers: only their products with the factor have to be fp32 numbers."""
+    for scale in (1e40, 1e-50):
+        picks, logits, dlogits, valid, _ = make(1, [90, 33], 24, 2, valid=0.8)
+        z = scale * 0.1 if score == "softmax" else 0.0
+        up = torch.tensor([1e-10 if scale > 1 else 1e30], device=DEV)
+        _, counts = call(picks, logits, dlogits, valid, 24, score, scale, z, up, loss=False)
+        _, grads, sizes = R.balance(np_lists(logits), np_valid(valid), to_np(counts), 2, score, scale, z, float(up))
+        for k in range(2):
+            expect_gradient(dlogits[0][k], grads[0][k], sizes[0][k], max(1.0, float(up) * scale * 100))
