@@ -197,7 +197,7 @@ struct Deal {
     }
 };
 
-// 2^x, 1/x and log x to 2 units in the last place of fp32, results below 2^-126 as 0: next to a row's largest score they are.
+// 2^x and 1/x to 2 units in the last place of fp32, results below 2^-126 as 0: next to a row's largest score they are.
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -513,7 +513,8 @@ __global__ void __launch_bounds__(kBlock, balance_ctas(C * V, SIG)) balance_kern
                 const float scale = empty ? 0.f : rcp_fast(total);
                 inner *= scale;
                 float lse = 0.f;
-                if (!SIG && P.z != 0.0) lse = empty ? 0.f : shift + __logf(total);
+                // (__logf is off by up to 2^-21 next to 1, where the sum is when one expert has most of it)
+                if (!SIG && P.z != 0.0) lse = empty ? 0.f : shift + logf(total);
                 if (live && q == 0) {
                     bal += inner;
                     zsum += (double)lse * lse;

@@ -91,3 +91,20 @@ def test_coefficients_past_fp32_with_a_small_factor(score):
         _, grads, sizes = R.balance(np_lists(logits), np_valid(valid), to_np(counts), 2, score, scale, z, float(up))
         for k in range(2):
             expect_gradient(dlogits[0][k], grads[0][k], sizes[0][k], max(1.0, float(up) * scale * 100))
+
+
+@pytest.mark.parametrize("experts", [2, 7, 64, 256])
+def test_z_loss_where_one_expert_has_nearly_everything(experts):
+    """Rows 0, -t, -infinity ...: lse = log(1 + exp(-t)), read off the z loss's gradient 2 / N lse p.  1 + exp(-t) is rounded by 2^-24 at
+    most; exp(-t) <= 0.0068 is off by 2^-19 of itself, the logarithm and the products by 2^-21 of lse <= 0.0068: 2^-25 together."""
+    n = 4096
+    t = torch.linspace(5, 12, n, device=DEV)
+    x = torch.full((n, experts), -float("inf"), device=DEV)
+    x[:, 0], x[:, -1] = 0, -t
+    d = torch.empty_like(x)
+    counts = torch.full((1, experts + 1), n, dtype=torch.int64, device=DEV)
+    routers = B.RouterSet(experts, logits=[[x]], dlogits=[[d]], topk=1)
+    B.ws_balance_loss(routers, counts, None, 0.0, 1.0, workspace=torch.empty(routers.workspace_bytes(), dtype=torch.uint8, device=DEV))
+    two = torch.stack([torch.zeros_like(t), -t], 1).double()
+    lse = d[:, 0].double() * (n / 2) / torch.softmax(two, 1)[:, 0]
+    assert float((lse - torch.logsumexp(two, 1)).abs().max()) <= 2.0 ** -24 + 2.0 ** -25
