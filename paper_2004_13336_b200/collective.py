@@ -37,7 +37,8 @@ class ShardedUpdate:
                  align_elems: int = 32, device=None, group=None, ops=None,
                  dropout: Optional[Tuple[float, int]] = None):
         """``dropout``: (p, seed).  Every replica then trains on its own random part of the weights: ``hand_out`` gives
-        it the first step's, each ``step`` takes the gradients of the present part and hands the next one out."""
+        it the first step's, each ``step`` takes the gradients of the present part and hands the next one out.  A
+        checkpoint holds ``drawn`` beside w, m and v."""
         if ops is None:
             from . import binding as ops      # fails loudly without the built CUDA library
         if opt not in ("sgdm", "adam", "lamb", "lars", "adafactor"):
@@ -65,12 +66,17 @@ class ShardedUpdate:
             self.fstate = torch.zeros(self.plan.factored_elems, **z)
 
     # -- sharding program (Section 4.2): every replica starts from the same full state -----
-    def load_state(self, w: Sequence[torch.Tensor], m: Sequence[torch.Tensor], v: Sequence[torch.Tensor]):
+    def load_state(self, w: Sequence[torch.Tensor], m: Sequence[torch.Tensor], v: Sequence[torch.Tensor],
+                   drawn: Optional[int] = None):
+        """``drawn``: with ``dropout``, the ``drawn`` of the run that the state is from, so that ``hand_out`` goes on with the
+        masks that this run would have drawn next (None: as it is, 0 in a new object)."""
         S, r = self.plan.S, self.rank
         full = torch.empty(self.plan.G, dtype=torch.float32, device=self.device)
         for src, dst in ((w, self.w), (m, self.m), (v, self.v)):
             self.ops.ws_pack(self.plan, src, full)
             dst.copy_(full[r * S:(r + 1) * S])
+        if drawn is not None:
+            self.drawn = drawn
 
     # -- unsharding program: the full slot tensors, for a checkpoint ------------------------
     def gather_slot(self, shard: torch.Tensor, out: Sequence[torch.Tensor]):
@@ -99,7 +105,7 @@ class ShardedUpdate:
 
     def hand_out(self, weights_out):
         """Gathers the present weights and hands this replica's part of them out, under the masks that the next
-        ``step``'s gradients belong to (with ``dropout`` only; ``self.drawn`` counts the steps)."""
+        ``step``'s gradients belong to (with ``dropout`` only): those of step ``self.drawn``, which counts the steps."""
         S, r = self.plan.S, self.rank
         self.gathered[r * S:(r + 1) * S].copy_(self.w)
         dist.all_gather_into_tensor(self.gathered, self.gathered[r * S:(r + 1) * S], group=self.group)
