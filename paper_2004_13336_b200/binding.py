@@ -76,6 +76,7 @@ class ws_tensor_table(C.Structure):
 class ws_dropout(C.Structure):
     _fields_ = [("p", C.c_double), ("seed", C.c_uint64), ("step", C.c_uint32), ("replica", C.c_int32),
                 ("step_dev", C.c_void_p)]
+    _keep = None                 # the tensor behind step_dev
 
 
 class ws_router_set(C.Structure):
@@ -741,10 +742,13 @@ def _on_current_device(t) -> int:
     return d
 
 
-def _check_flat(plan, r, flat):
+def _check_flat(plan, r, flat, table, drop):
     """ws_unpack_dropout and ws_reduce_dropout take a whole layout or one shard by ``r``: its size is all that tells a
-    buffer of the other kind from the right one."""
+    buffer of the other kind from the right one.  What the kernels read beside it lies on its device."""
     device = _on_current_device(flat)
+    for buf in (plan.dev_buf, getattr(table, "dev_buf", None), drop._keep):
+        if buf is not None and buf.get_device() != device:
+            raise ValueError(f"plan, tables and step_dev on {flat.device} expected, not on {buf.device}")
     want = plan.G if r < 0 else plan.S
     if flat.numel() != want or not flat.is_contiguous():
         raise ValueError(f"flat is a contiguous buffer of {want} elements for r = {r}, not {tuple(flat.shape)}")
@@ -756,7 +760,7 @@ def ws_unpack_dropout(plan: Plan, r: int, flat: torch.Tensor, lists: TensorTable
     if type(lists.c) is not ws_tensor_table or type(drop) is not ws_dropout:
         for x, cls in ((lists.c, ws_tensor_table), (drop, ws_dropout)):
             _refuse(x, cls)
-    device = _check_flat(plan, r, flat)
+    device = _check_flat(plan, r, flat, lists, drop)
     st = _step().ws_unpack_dropout(plan.handle, r, flat.data_ptr(), _dtype_code(flat.dtype), C.addressof(lists.c),
                                    C.addressof(drop), _raw_stream(device))
     if st:
@@ -768,7 +772,7 @@ def ws_reduce_dropout(plan: Plan, r: int, grads: TensorTable, drop: ws_dropout, 
     if type(grads.c) is not ws_tensor_table or type(drop) is not ws_dropout:
         for x, cls in ((grads.c, ws_tensor_table), (drop, ws_dropout)):
             _refuse(x, cls)
-    device = _check_flat(plan, r, flat)
+    device = _check_flat(plan, r, flat, grads, drop)
     st = _step().ws_reduce_dropout(plan.handle, r, C.addressof(grads.c), C.addressof(drop), flat.data_ptr(),
                                    _dtype_code(flat.dtype), _raw_stream(device))
     if st:
