@@ -8,6 +8,7 @@ streams come from ``torch.cuda.current_stream()``.
 from __future__ import annotations
 
 import ctypes as C
+import operator
 import os
 import struct
 from array import array
@@ -713,18 +714,28 @@ def ws_pack_sets(plan: Plan, table: TensorTable, flats):
         raise WsError(st, "ws_pack_sets")
 
 
+def _int32(n, what) -> int:
+    """ctypes keeps the low 32 bits of a number: one that needs more would pass for another."""
+    n = operator.index(n)
+    if not -(1 << 31) <= n < 1 << 31:
+        raise ValueError(f"{what} is a number of 32 bits, not {n}")
+    return n
+
+
 def make_dropout(p: float, seed: int, step: int = 0, replica: int = 0,
                  step_dev: Optional[torch.Tensor] = None) -> ws_dropout:
     """Dropout of probability ``p`` for ws_unpack_dropout and ws_reduce_dropout: masks of the run ``seed`` and the
     training step ``step``; a table's first set belongs to ``replica``.  ``step_dev``: a device tensor of one 32-bit
-    integer that the kernels add to ``step``, for captured steps; the caller keeps it alive."""
+    integer that the kernels add to ``step``, for captured steps; the caller keeps it alive.  ``seed`` counts modulo 2^64 and
+    ``step`` modulo 2^32; a replica's number has to be one of 32 bits (the calls refuse what is not below 65536)."""
+    replica = _int32(int(replica), "replica")
     if step_dev is not None:
         if step_dev.dtype not in (torch.int32, torch.uint32) or step_dev.numel() != 1 or not step_dev.is_cuda:
             raise TypeError("step_dev is a device tensor of one 32-bit integer")
-        d = ws_dropout(float(p), int(seed) & 0xFFFFFFFFFFFFFFFF, int(step) & 0xFFFFFFFF, int(replica), step_dev.data_ptr())
+        d = ws_dropout(float(p), int(seed) & 0xFFFFFFFFFFFFFFFF, int(step) & 0xFFFFFFFF, replica, step_dev.data_ptr())
         d._keep = step_dev
         return d
-    return ws_dropout(float(p), int(seed) & 0xFFFFFFFFFFFFFFFF, int(step) & 0xFFFFFFFF, int(replica))
+    return ws_dropout(float(p), int(seed) & 0xFFFFFFFFFFFFFFFF, int(step) & 0xFFFFFFFF, replica)
 
 
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)      # (without the Python around it)
@@ -746,6 +757,8 @@ def _check_flat(plan, r, flat, table, drop):
     """ws_unpack_dropout and ws_reduce_dropout take a whole layout or one shard by ``r``: its size is all that tells a
     buffer of the other kind from the right one.  What the kernels read beside it lies on its device."""
     device = _on_current_device(flat)
+    if not -1 <= r < plan.R:
+        raise ValueError(f"r is -1 or a shard below {plan.R}, not {r}")
     for buf in (plan.dev_buf, getattr(table, "dev_buf", None), drop._keep):
         if buf is not None and buf.get_device() != device:
             raise ValueError(f"plan, tables and step_dev on {flat.device} expected, not on {buf.device}")
@@ -793,9 +806,10 @@ class RouterSet:
             raise ValueError("a router set has picks or logits of one layer and one replica at least")
         if any(t.dim() != 2 for t in like[0]):
             raise ValueError("picks and logits have a row for every token")
+        experts = _int32(experts, "experts")
         layers, replicas = len(like), len(like[0])
         tokens = [t.shape[0] for t in like[0]]
-        self.experts, self.layers, self.replicas = int(experts), layers, replicas
+        self.experts, self.layers, self.replicas = experts, layers, replicas
         self.device = like[0][0].device
         c = self.c = ws_router_set(layers=layers, replicas=replicas, experts=experts, topk=1)
         self._keep = keep = []
@@ -824,7 +838,7 @@ class RouterSet:
             return lds.pop()
 
         if topk is not None:
-            c.topk = topk
+            c.topk = topk = _int32(topk, "topk")
         elif picks is None:
             raise ValueError("a router set without picks needs topk")
         if picks is not None:

@@ -67,3 +67,22 @@ def test_buffers_of_another_device(calls):
         with pytest.raises(ValueError):
             calls(**bad)
     assert calls() == 6
+
+
+def test_numbers_that_32_bits_do_not_hold(calls):
+    """Each would pass for a small one by its low 32 bits."""
+    big = 1 << 32
+    for replica in (big, big + 5, 1 << 31, -(1 << 31) - 1, 1 << 40):
+        with pytest.raises(ValueError):
+            B.make_dropout(0.1, 3, 0, replica)
+    for r in (-2, 4, big, big + 1, big - 1, -big):
+        with pytest.raises(ValueError):
+            calls(r=r)
+    q, x = [[torch.zeros(3, 2, dtype=torch.int64)]], [[torch.zeros(3, 8)]]
+    for bad in (lambda: B.RouterSet(big + 8, q), lambda: B.RouterSet(8, logits=x, topk=big + 2), lambda: B.RouterSet(-big + 8, q)):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: B.RouterSet(8.0, q), lambda: B.RouterSet(8, logits=x, topk=2.0)):
+        with pytest.raises(TypeError):
+            bad()
+    assert B.make_dropout(0.1, 3, 0, 65535).replica == 65535 and B.RouterSet(8, logits=x, topk=2).c.topk == 2
