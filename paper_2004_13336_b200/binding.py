@@ -904,18 +904,21 @@ def ws_balance_loss(routers: RouterSet, counts: torch.Tensor, loss: Optional[tor
                     upstream: Optional[torch.Tensor] = None, accumulate: bool = False,
                     workspace: Optional[torch.Tensor] = None):
     """The load-balancing loss and the z loss of every layer (loss[l][0], loss[l][1]) and, into the set's dlogits, the
-    gradient of ``upstream`` (a device float, else 1) times their sum by the logits."""
+    gradient of ``upstream`` (a device float, else 1) times their sum by the logits.  ``workspace``: scratch of
+    ``routers.workspace_bytes()`` bytes, one for each call that can run at the same time; None takes it from torch's
+    allocator for this call."""
     addr = _router_addr(routers, counts)
     if loss is not None and (loss.dtype is not torch.float32 or loss.shape != routers._loss_shape or not loss.is_contiguous()
                              or loss.get_device() != routers._index):
         raise ValueError(f"loss: a contiguous float32 tensor [{routers.layers}, 2] beside the routers' tensors")
     if upstream is not None and (upstream.dtype is not torch.float32 or upstream.numel() != 1 or upstream.get_device() != routers._index):
         raise TypeError("upstream: a tensor of one float32 beside the routers' tensors")
-    if workspace is not None and workspace.get_device() != routers._index:
+    if workspace is None:
+        workspace = torch.empty(routers.workspace_bytes(), dtype=torch.uint8, device=counts.device)
+    elif workspace.get_device() != routers._index:
         raise ValueError("workspace: a tensor beside the routers' tensors")
     st = _step().ws_balance_loss(addr, counts.data_ptr(), loss.data_ptr() if loss is not None else None, coef, z_coef,
                                  upstream.data_ptr() if upstream is not None else None, 1 if accumulate else 0,
-                                 workspace.data_ptr() if workspace is not None else None,
-                                 workspace.nbytes if workspace is not None else 0, _raw_stream(routers._index))
+                                 workspace.data_ptr(), workspace.nbytes, _raw_stream(routers._index))
     if st:
         raise WsError(st, "ws_balance_loss")

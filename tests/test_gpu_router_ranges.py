@@ -108,3 +108,27 @@ def test_z_loss_where_one_expert_has_nearly_everything(experts):
     two = torch.stack([torch.zeros_like(t), -t], 1).double()
     lse = d[:, 0].double() * (n / 2) / torch.softmax(two, 1)[:, 0]
     assert float((lse - torch.logsumexp(two, 1)).abs().max()) <= 2.0 ** -24 + 2.0 ** -25
+
+
+def test_balance_loss_finds_its_own_scratch():
+    """Without a workspace, eager and captured: the same bits as with one."""
+    picks, logits, dlogits, valid, _ = make(3, [5000, 17], 64, 2, valid=0.8)
+    want, counts = call(picks, logits, dlogits, valid, 64, z=1e-3)
+    first = [t.clone() for layer in dlogits for t in layer]
+    routers = B.RouterSet(64, picks, valid, logits, dlogits)
+    loss = torch.empty_like(want)
+    B.ws_balance_loss(routers, counts, loss, 1e-2, 1e-3)
+    assert torch.equal(loss, want)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.ws_balance_loss(routers, counts, loss, 1e-2, 1e-3)
+    for _ in range(2):
+        loss.fill_(9)
+        for layer in dlogits:
+            for t in layer:
+                t.fill_(9)
+        graph.replay()
+        assert torch.equal(loss, want) and all(torch.equal(a, b) for a, b in zip(first, (t for layer in dlogits for t in layer)))
+    with pytest.raises(B.WsError):
+        B.ws_balance_loss(B.RouterSet(64, picks), counts, loss, 1e-2)          # no logits
