@@ -86,11 +86,6 @@ __device__ __forceinline__ void store8(void* base, long long e, const Fv<8>& x) 
         store_f32<4>((float*)base + e + 4, Fv<4>{x.f[4], x.f[5], x.f[6], x.f[7]});
     }
 }
-template <bool BF>
-__device__ __forceinline__ void store8_partial(void* base, long long e, const Fv<8>& x, int n) {
-    if constexpr (BF) store_bf16_partial<8>((unsigned short*)base + e, x, n);
-    else store_f32_partial<8>((float*)base + e, x, n);
-}
 
 // What a launch's item is: its tile, where it lies in `flat` and in the tensor.
 struct DropItem {
@@ -358,10 +353,14 @@ void launch_op(bool sum, void* flat, const Shape& s, cudaStream_t st, const Drop
     if (!sum) {
         // Four vectors in flight need tiles that have them; without, with many lists, a draw's latency is all there is (us, 4 / 1:
         // 16 lists of 2 M in 64 shards 50 / 29, in 16 shards 42 / 23, 3 lists of 45 M in 64 shards 66 / 72).
-        if (FBF && TBF && (P.nsets <= 3 || s.average >= 1536)) launch_tiles(hand_out_kernel<FBF, TBF, WIDE, SHORT, 4, 5>, s, 64, 4, st, P, from);
-        else if (FBF && TBF) launch_tiles(hand_out_kernel<FBF, TBF, WIDE, SHORT, 1, 5>, s, 64, 1, st, P, from);
-        else if (P.nsets == 1) launch_tiles(hand_out_kernel<FBF, TBF, WIDE, SHORT, 2, 3>, s, 64, 2, st, P, from);
-        else launch_tiles(hand_out_kernel<FBF, TBF, WIDE, SHORT, 2, 1>, s, 128, 2, st, P, from);
+        if constexpr (FBF && TBF) {
+            if (P.nsets <= 3 || s.average >= 1536) launch_tiles(hand_out_kernel<true, true, WIDE, SHORT, 4, 5>, s, 64, 4, st, P, from);
+            else launch_tiles(hand_out_kernel<true, true, WIDE, SHORT, 1, 5>, s, 64, 1, st, P, from);
+        } else if (P.nsets == 1) {
+            launch_tiles(hand_out_kernel<FBF, TBF, WIDE, SHORT, 2, 3>, s, 64, 2, st, P, from);
+        } else {
+            launch_tiles(hand_out_kernel<FBF, TBF, WIDE, SHORT, 2, 1>, s, 128, 2, st, P, from);
+        }
     } else if (P.nsets == 1) {
         launch_tiles(sum_kernel<FBF, TBF, WIDE, SHORT, 1, 2, false, TBF ? 5 : 4>, s, 64, 2, st, P, flat);
     } else if (P.nsets == 2) {
