@@ -21,10 +21,13 @@ constexpr int kBlock = 256;
 template <int NP, int NR>
 struct RouterTab {
     const void* in[NP];            // [layers of the launch][replicas] picks or logits
-    void* out[NP];                 // ... dlogits
     const unsigned char* valid[NR];// [replicas]
     int tokens[NR];                // [replicas]
     int chunk0[NR];                // [replicas] first chunk of a replica's tokens
+};
+template <int NP, int NR>
+struct BalanceTab : RouterTab<NP, NR> {
+    void* out[NP];                 // [layers of the launch][replicas] dlogits
 };
 
 struct RouterParams {
@@ -336,7 +339,7 @@ __host__ __device__ constexpr int balance_ctas(int elems, bool sig) {
 // X: the logits' type.  A row lies on P.lanes lanes; lane q holds the C vectors of V elements at (c lanes + q) V.
 template <typename X, int V, int C, bool SIG, int NP, int NR>
 __global__ void __launch_bounds__(kBlock, balance_ctas(C * V, SIG)) balance_kernel(const __grid_constant__ BalanceParams P, const Deal deal,
-                                                                                   const __grid_constant__ RouterTab<NP, NR> tab) {
+                                                                                   const __grid_constant__ BalanceTab<NP, NR> tab) {
     constexpr int N = C * V, H = (N + 1) / 2;             // elements of a lane, pairs
     __shared__ __align__(16) float shares[kMaxExperts];       // (32 lanes hold at most 32 elements each)
     __shared__ double2 part[kBlock / 32];
@@ -653,11 +656,8 @@ long long chunks_of(const ws_router_set* s, long long rows) {
     return n > 0 ? n : 1;
 }
 template <int NP, int NR>
-void fill(RouterTab<NP, NR>& tab, const ws_router_set* s, const void* const* in, void* const* out, int layer0, int layers, int rows) {
-    for (int i = 0; i < layers * s->replicas; ++i) {
-        tab.in[i] = in ? in[(long long)layer0 * s->replicas + i] : nullptr;
-        tab.out[i] = out ? out[(long long)layer0 * s->replicas + i] : nullptr;
-    }
+void fill(RouterTab<NP, NR>& tab, const ws_router_set* s, const void* const* in, int layer0, int layers, int rows) {
+    for (int i = 0; i < layers * s->replicas; ++i) tab.in[i] = in[(long long)layer0 * s->replicas + i];
     int at = 0;
     for (int k = 0; k < s->replicas; ++k) {
         tab.valid[k] = s->valid ? s->valid[k] : nullptr;
@@ -671,7 +671,7 @@ void fill(RouterTab<NP, NR>& tab, const ws_router_set* s, const void* const* in,
 template <int NP, int NR>
 void launch_counts(const ws_router_set* s, const RouterParams& P, int layers, int ctas, bool cluster, int64_t* counts, int accumulate, cudaStream_t st) {
     RouterTab<NP, NR> tab;
-    fill(tab, s, s->picks, nullptr, P.layer0, layers, P.rows);
+    fill(tab, s, s->picks, P.layer0, layers, P.rows);
     const dim3 grid(ctas, layers);
     long long* out = (long long*)counts;
     if (cluster) {
@@ -684,7 +684,7 @@ void launch_counts(const ws_router_set* s, const RouterParams& P, int layers, in
 }
 
 template <typename X, int V, int C, int NP, int NR>
-Deal launch_score(const ws_router_set* s, const BalanceParams& P, const RouterTab<NP, NR>& tab, cudaStream_t st) {
+Deal launch_score(const ws_router_set* s, const BalanceParams& P, const BalanceTab<NP, NR>& tab, cudaStream_t st) {
     const bool sig = s->score == WS_SIGMOID;
     const long long items = (long long)P.layers * (P.whole ? 1 : P.r.chunks), most = (long long)P.sms * balance_ctas(C * V, sig);
     const int grid = (int)(items < most ? items : most < kMaxCtas ? most : kMaxCtas);
@@ -697,7 +697,7 @@ Deal launch_score(const ws_router_set* s, const BalanceParams& P, const RouterTa
 // ones (rows off the 16-byte boundaries: bf16 rows of 60, 15.7 M, 41 us, with 2 elements 77, with 16 40; fp32 rows of 33 29, 55, 30),
 // more where 32 lanes do not hold the row that way.  Short fp32 rows keep two lanes side by side (rows of 16 20 -> 17; bf16 16 -> 19).
 template <typename X, int NP, int NR>
-Deal launch_shape(const ws_router_set* s, bool wide, BalanceParams& P, const RouterTab<NP, NR>& tab, cudaStream_t st) {
+Deal launch_shape(const ws_router_set* s, bool wide, BalanceParams& P, const BalanceTab<NP, NR>& tab, cudaStream_t st) {
     constexpr int V = 16 / sizeof(X);
     const int vecs = wide ? s->experts / V : s->experts;
     int c = 1;
@@ -720,8 +720,9 @@ Deal launch_shape(const ws_router_set* s, bool wide, BalanceParams& P, const Rou
 }
 template <int NP, int NR>
 Deal launch_balance(const ws_router_set* s, bool wide, BalanceParams& P, cudaStream_t st) {
-    RouterTab<NP, NR> tab;
-    fill(tab, s, s->logits, s->dlogits, P.r.layer0, P.layers, P.r.rows);
+    BalanceTab<NP, NR> tab;
+    fill(tab, s, s->logits, P.r.layer0, P.layers, P.r.rows);
+    for (int i = 0; i < P.layers * s->replicas; ++i) tab.out[i] = s->dlogits ? s->dlogits[(long long)P.r.layer0 * s->replicas + i] : nullptr;
     return s->dtype == WS_F32 ? launch_shape<float>(s, wide, P, tab, st) : launch_shape<__nv_bfloat16>(s, wide, P, tab, st);
 }
 
