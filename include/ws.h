@@ -664,7 +664,8 @@ ws_status ws_reduce_dropout(const ws_plan* plan, int32_t r, const ws_tensor_tabl
  * ws_balance_loss reads them and writes loss ([layers][2] floats, device, or NULL) and dlogits; with
  * `accumulate` it adds the gradient to what dlogits holds (in fp32, rounded once).  A logit of -infinity is
  * an expert that the token cannot pick, with score and gradient 0; a row of nothing else has no scores, adds
- * nothing to either loss and has gradient 0.  NaN or (WS_SOFTMAX) +infinity in a valid row gives NaN.  A layer
+ * nothing to either loss and has gradient 0.  Scores are fp32 numbers: one below 2^-126 counts as 0 (with
+ * WS_SOFTMAX, and with WS_SIGMOID in rows whose scores add up to less than 1e-17, in relation to the largest).  NaN or (WS_SOFTMAX) +infinity in a valid row gives NaN.  A layer
  * without tokens has loss and gradient 0.
  *   coef, z_coef  finite; z_coef must be 0 with WS_SIGMOID
  *   upstream      device float u, or NULL for 1.  u coef experts / N and u z_coef / N are formed in 64 bits; where

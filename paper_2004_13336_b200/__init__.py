@@ -16,7 +16,7 @@ of the C functions::
     ws.ws_unpack_dropout(plan, -1, w, tables, ws.make_dropout(p, seed, step))     # each replica its own random part
     ws.ws_reduce_dropout(plan, -1, grad_tables, drop, summed)         # ... and their gradients' sum, one copy for the update
     ws.ws_router_counts(routers, counts)                              # balance of a model's experts over all replicas
-    ws.ws_balance_loss(routers, counts, loss, coef, workspace=scratch)
+    ws.ws_balance_loss(routers, counts, loss, coef)                   # routers: a ws.RouterSet, made once
 
 ``workloads.py`` holds the model-shaped synthetic tensor sets used by the
 tests and the benchmark.  There is no CPU fallback: without the built library

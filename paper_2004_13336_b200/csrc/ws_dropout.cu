@@ -343,16 +343,17 @@ void launch_tiles(Kernel kernel, const Shape& s, int most, int unroll, cudaStrea
 // per block of 8 elements and set, and a comparison and a choice per element.  On bf16 tensors that is 10 instructions an
 // element, half of them of the integer pipe's half rate, near what the copy leaves time for; fp32 tensors have twice the time.
 // So small CTAs (a long tile's latencies overlap with other tiles'), registers for many of them, no more loads in flight than
-// that needs.  us by threads of a CTA, 335 M elements from bf16 to one bf16 list: 256 249, 128 225, 64 213 (205 at the copy
-// bandwidth); the sum of one bf16 list 260 / 237 / 228, of 2 of 61 M 89 / 89 / 79 (75), of 4 of 1.56 G 2916 / 2920 / 2972
-// (2859); 4 bf16 lists from an fp32 state of 451 M 899 / 857 / 887 (828).  With 3 CTAs of 256 instead of 6 the sum
-// of 4 lists takes 3275.  More than 8 bf16 lists: blocks of 8 halve the compensation's steps, 16 lists of 61 M 460 -> 399 (338).
+// that needs.  us in runs of 0.6 s, whose power takes the SM clock from 1.96 GHz to 1.6 to 1.8, by threads of a CTA: 335 M elements
+// from bf16 to one bf16 list 256 264, 128 241, 64 231 (205 at the copy bandwidth; 216 in runs of 60 ms); the sum of one bf16
+// list 259 / 244 / 240, of 2 of 61 M 91 / 91 / 83 (75), of 4 of 1.56 G 3186 / 3116 / 3118 (2859); 4 bf16 lists from an fp32
+// state of 451 M 960 / 883 / 908 (828).  With 3 CTAs of 256 an SM the sum of 4 lists takes 3378.  More than 8 bf16
+// lists: blocks of 8 halve the compensation's steps, 16 lists of 61 M 476 -> 438 (338).
 template <bool FBF, bool TBF, bool WIDE, bool SHORT>
 void launch_op(bool sum, void* flat, const Shape& s, cudaStream_t st, const DropParams& P) {
     const void* from = flat;
     if (!sum) {
         // Four vectors in flight need tiles that have them; without, with many lists, a draw's latency is all there is (us, 4 / 1:
-        // 16 lists of 2 M in 64 shards 50 / 29, in 16 shards 42 / 23, 3 lists of 45 M in 64 shards 66 / 72).
+        // 16 lists of 2 M in 64 shards 50 / 29, in 16 shards 42 / 24, 3 lists of 45 M in 64 shards 70 / 74).
         if constexpr (FBF && TBF) {
             if (P.nsets <= 3 || s.average >= 1536) launch_tiles(hand_out_kernel<true, true, WIDE, SHORT, 4, 5>, s, 64, 4, st, P, from);
             else launch_tiles(hand_out_kernel<true, true, WIDE, SHORT, 1, 5>, s, 64, 1, st, P, from);
@@ -423,8 +424,8 @@ ws_status run(bool sum, const ws_plan* p, int32_t r, void* flat, ws_dtype flat_d
 #endif
     const bool wide = table->min_align >= 32 && (reinterpret_cast<uintptr_t>(flat) & 31u) == 0;
     // A warp per tile where tiles are short and many, and not long enough in any place to leave a warp walking alone (ws_pack's
-    // rule, in elements).  us, a CTA / a warp per tile: 64 shards of 47 M in tiles of 900, sum of one bf16 list 56 / 40, fp32 to one
-    // list 61 / 60; 16 bf16 lists of 4 M in tiles of 660, whose draws are enough work for a CTA, 38 / 50, 8 of 2 M 15 / 22.
+    // rule, in elements).  us, a CTA / a warp per tile: 64 shards of 47 M in tiles of 900, sum of one bf16 list 56 / 42, fp32 to one
+    // list 64 / 61; 16 bf16 lists of 4 M in tiles of 660, whose draws are enough work for a CTA, 42 / 53, 8 of 2 M 15 / 22.
     const long long tile = p->ntiles > 0 ? (P.concat ? p->S * p->R : p->S) / p->ntiles : p->K;
     const Shape s{P.nitems, p->K, tile, P.nitems > 32LL * p->sms && tile <= (P.nsets <= 2 ? 1024 : P.nsets <= 4 ? 768 : 256) && p->longest <= 128 << 10};
     cudaStream_t st = (cudaStream_t)stream;

@@ -325,11 +325,11 @@ __device__ __forceinline__ void row_sum2(float& a, float& b, int G) {
 
 // The rows' pass.  Its floor is the copy of the logits; what it has to do per element meanwhile is an exponential, a few
 // packed additions and products and, with bf16, taking the pairs apart and putting them together, and per row three sums over
-// its lanes (17 instructions an element of bf16 rows of 64, where 22 fit into the copy's time).  So a lane holds 16 elements where a row
+// its lanes (18 instructions an element of bf16 rows of 64, where 22 fit into the copy's time).  So a lane holds 16 elements where a row
 // has so many, the launch is one wave of CTAs that walk runs of consecutive rows (the counts are read once a layer and CTA), and the next
-// row is on its way while the present one is worked on.  us: 43 M bf16 logits in rows of 64 (24 layers, 8 replicas, z loss) 39,
+// row is on its way while the present one is worked on.  us: 43 M bf16 logits in rows of 64 (24 layers, 8 replicas, z loss) 40,
 // 26 at the copy bandwidth (lanes of 8 elements 48, CTAs of 64 KB instead of one wave 58, single fp32 instructions 48); 134 M
-// fp32 sigmoid logits in rows of 256 176, 164 at the copy bandwidth (CTAs of 64 KB 264).
+// fp32 sigmoid logits in rows of 256 177, softmax 189, 164 at the copy bandwidth (sigmoid in CTAs of 64 KB 264).
 //
 // Resident CTAs per SM by the elements of a lane.
 __host__ __device__ constexpr int balance_ctas(int elems, bool sig) {
@@ -775,7 +775,7 @@ extern "C" ws_status ws_router_counts(const ws_router_set* s, int64_t* counts, i
     // Chunks of about 512 picks, one for a warp; a power of two of tokens, so that chunks of aligned picks are aligned.
     // A cluster of up to 8 CTAs a layer, while none of its warps has more than 2 chunks.  us, a cluster / chunks of 8192 picks:
     // 24 layers of 65 K picks 6.8 / 11, 1 of 65 K 5.3 / 7.4, 48 of 33 K 5.9 / 16; 1 of 262 K 13.2 / 6.3, 8 of 262 K 19 / 8.2
-    // (what bounds it is a CTA's counting, 2 picks a cycle).  4 layers of 2.1 M 64-bit picks, chunks of 8192 / 16384: 19.5 / 17.6.
+    // (a cluster's few CTAs count some 2 picks a cycle each).  4 layers of 2.1 M 64-bit picks, chunks of 8192 / 16384: 19.5 / 17.6.
     P.rows = 4;
     while (2 * P.rows * s->topk <= 512) P.rows *= 2;
     long long chunks = chunks_of(s, P.rows);
