@@ -178,10 +178,11 @@ class ExpertBalance:
 
     def step(self, routers, upstream: Optional[torch.Tensor] = None, accumulate: bool = False) -> torch.Tensor:
         """``routers``: this replica's tensors (``ops.RouterSet``, with one replica's lists).  Fills their dlogits and
-        returns the batch's losses [layers][2], a new tensor for each call; ``self.counts`` holds the batch's counts until
-        the next one, the tokens' number last."""
+        returns the batch's losses [layers][2]; ``self.counts`` are the batch's counts, the tokens' number last.  Both are new
+        tensors for each call, a captured step's its own: steps captured apart may be replayed at the same time."""
         # scratch of this call: one kept here and replaced by a larger one would be gone under a captured step
         workspace = torch.empty(max(16, routers.workspace_bytes()), dtype=torch.uint8, device=self.counts.device)
+        self.counts = torch.empty_like(self.counts)
         self.ops.ws_router_counts(routers, self.counts)
         dist.all_reduce(self.counts, group=self.group)
         self.loss = torch.empty_like(self.loss)

@@ -127,3 +127,29 @@ def test_replayed_balance_keeps_to_its_own_memory(world_of_one):
         assert all(bool((t == 0x5A).all()) for t in others)
     finally:
         graph.reset()
+
+
+def test_steps_captured_apart_share_nothing(world_of_one):
+    """Two steps of one object, captured apart: each replay leaves the other's counts and losses alone."""
+    from paper_2004_13336_b200 import binding as B
+    from paper_2004_13336_b200.collective import ExpertBalance
+    balance = ExpertBalance(2, 64, 0.01, 1e-3)
+    sets = [_routers(B, n, 64, seed) for n, seed in ((3000, 3), (2500, 4))]
+    want = [(balance.step(s).clone(), balance.counts.clone()) for s in sets]
+    torch.cuda.synchronize()
+    graphs, got = [torch.cuda.CUDAGraph() for _ in sets], []
+    try:
+        for g, s in zip(graphs, sets):
+            with torch.cuda.graph(g, capture_error_mode="thread_local"):
+                loss = balance.step(s)
+            got.append((loss, balance.counts))
+        for order in ((0, 1), (1, 0)):
+            for x in got:
+                x[0].fill_(9)
+                x[1].fill_(9)
+            for i in order:
+                graphs[i].replay()
+            assert all(torch.equal(a, b) for x, y in zip(got, want) for a, b in zip(x, y))
+    finally:
+        for g in graphs:
+            g.reset()
